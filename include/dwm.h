@@ -446,6 +446,93 @@ DWM_API dwm_status_t dwm_bf16_input_transform(const dwm_bf16_plan_t* plan, const
 DWM_API dwm_status_t dwm_bf16_contract_output(const dwm_bf16_plan_t* plan, const dwm_bf16_t* U_dev,
                                               dwm_bf16_t* y_dev, void* stream);
 
+/*
+ * Layer norm, dropout, and the join of a residual branch: what stands before and behind the convolutions of a block, in
+ * training and in serving.  Storage types are those of the convolutions; parameters (gamma, beta and their gradients) are
+ * binary32 or of the tensors' type; statistics and sums are binary32.
+ *
+ * Tensors are [outer][C][inner], element (o, c, i) at o*stride + c*inner + i, and a norm goes over the C channels of one
+ * (o, i): with inner = 1 over the rows of an [outer][C] matrix (tokens, pooled features), with inner = H*W over the channels of
+ * every pixel of [N][C][H][W] maps, as the convolutions write and read them.
+ *     mean = (1/C) sum_c x,  rstd = 1 / sqrt((1/C) sum_c (x - mean)^2 + eps),  y = (x - mean) * rstd * gamma[c] + beta[c]
+ * mean and rstd are [outer][inner].  Values of up to about 1e19 / sqrt(C) from their mean can be normed (their squares are
+ * summed in binary32); infinities and NaN make their own norm's y, mean and rstd NaN or infinite, and no other's.
+ *
+ * Memory and streams as for the convolutions: plans are host memory; everything else is the caller's device memory, at
+ * multiples of its element's size; nothing is allocated or synchronised; kernels go to `stream`; errors are return codes; calls
+ * can be captured into a HIP graph.  Calls that use the same plan's workspace (the backward ones) must be ordered on one
+ * stream.  Outputs overlap nothing, except that an output may be the very memory, with the same stride, of one input: y of x in
+ * dwm_norm_forward and dwm_dropout_forward, z of residual, dx of dy, dresidual of dz.  Results do not vary from run to run.
+ */
+typedef enum { DWM_F32 = 0, DWM_F16 = 1, DWM_BF16 = 2 } dwm_type_t;
+
+/* Which elements are dropped, and without a mask in memory: element e of a tensor in its dense order ((o*C + c)*inner + i,
+ * whatever the strides) takes word e % 4 of the block that Philox-4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, SC 2011)
+ * makes of the counter (e / 4, sequence) under the key seed, and is dropped where that word is below p * 2^32.  The backward call
+ * takes the same values and draws the same mask.  Masks of different (seed, sequence) are independent: a program counts sequence
+ * up from call to call, or, where calls are replayed from a graph, the number at sequence_dev (added to sequence when the
+ * kernel runs).  A kept element is multiplied by 1 / (1 - p), rounded to binary32; a dropped one becomes zero whatever it
+ * held, infinities and NaN too; p = 1 drops all. */
+typedef struct {
+    double p;                               /* 0 <= p <= 1 */
+    unsigned long long seed, sequence;
+    const unsigned long long* sequence_dev; /* NULL, or device memory, 8-byte aligned */
+} dwm_dropout_t;
+
+/* y[e] = kept(e) ? x[e] / (1 - p) : 0, over n elements (n = 0: nothing to do); dx the same of dy. */
+DWM_API dwm_status_t dwm_dropout_forward(const dwm_dropout_t* drop, dwm_type_t type, long long n, const void* x_dev,
+                                         void* y_dev, void* stream);
+DWM_API dwm_status_t dwm_dropout_backward(const dwm_dropout_t* drop, dwm_type_t type, long long n, const void* dy_dev,
+                                          void* dx_dev, void* stream);
+
+typedef struct dwm_norm_plan dwm_norm_plan_t;
+
+typedef struct {
+    long long outer;
+    int C;
+    long long inner;
+    int forward_kernel, backward_kernel; /* 0: the kernels for any size */
+    int splits;                          /* parts of the positions whose sums of the parameters' gradients are added up last */
+} dwm_norm_info_t;
+
+/* outer >= 0 (0: calls write no tensor; gradients of parameters become zero), C >= 1, inner >= 1, eps >= 0 and finite; param_type is
+ * DWM_F32 or type.  DWM_ERR_UNSUPPORTED for C above 2^20 or more than 2^40 elements.  Host only. */
+DWM_API dwm_status_t dwm_norm_plan_create(dwm_norm_plan_t** out, long long outer, int C, long long inner, dwm_type_t type,
+                                          dwm_type_t param_type, double eps);
+DWM_API dwm_status_t dwm_norm_plan_destroy(dwm_norm_plan_t* plan);
+DWM_API dwm_status_t dwm_norm_plan_info(const dwm_norm_plan_t* plan, dwm_norm_info_t* info);
+/* Elements between one o and the next of a tensor ("x", "residual", "z", "y", "dy", "dz", "dx", "dresidual"): at least C*inner,
+ * which is the default; more where a tensor is a slice of a wider one.  May be called at any time. */
+DWM_API dwm_status_t dwm_norm_set_stride(dwm_norm_plan_t* plan, const char* tensor, long long stride);
+/* The workspace holds partial sums of dgamma and dbeta: 256-byte aligned, needed by backward calls that are asked for one of
+ * them and by no other call. */
+DWM_API size_t dwm_norm_workspace_bytes(const dwm_norm_plan_t* plan);
+DWM_API dwm_status_t dwm_norm_set_workspace(dwm_norm_plan_t* plan, void* ws_dev, size_t bytes);
+
+/* gamma and beta may be NULL (ones, zeros), mean and rstd too (serving). */
+DWM_API dwm_status_t dwm_norm_forward(const dwm_norm_plan_t* plan, const void* x_dev, const void* gamma_dev,
+                                      const void* beta_dev, void* y_dev, float* mean_dev, float* rstd_dev, void* stream);
+/* With xhat = (x - mean) * rstd and g = dy * gamma:
+ *     dx = rstd * (g - (1/C) sum_c g - xhat * (1/C) sum_c g*xhat),  dgamma = sum_{o,i} dy*xhat,  dbeta = sum_{o,i} dy
+ * each overwritten; any of the three may be NULL and is then not computed, but not all of them. */
+DWM_API dwm_status_t dwm_norm_backward(const dwm_norm_plan_t* plan, const void* dy_dev, const void* x_dev,
+                                       const void* gamma_dev, const float* mean_dev, const float* rstd_dev, void* dx_dev,
+                                       void* dgamma_dev, void* dbeta_dev, void* stream);
+/* A branch x joined to its residual stream, and the next norm, in one pass:
+ *     z = residual + dropout(x),  y = norm(z)
+ * the product and the sum rounded to binary32 each, then z to its type; the norm reads z as it is stored.  drop may be NULL
+ * (serving): z = residual + x. */
+DWM_API dwm_status_t dwm_norm_join_forward(const dwm_norm_plan_t* plan, const dwm_dropout_t* drop, const void* x_dev,
+                                           const void* residual_dev, const void* gamma_dev, const void* beta_dev, void* z_dev,
+                                           void* y_dev, float* mean_dev, float* rstd_dev, void* stream);
+/* dz is the gradient that reaches z from elsewhere, along the residual stream (NULL: none):
+ *     dresidual = dz + (dx of dwm_norm_backward, of dy and z),  dx = dropout of that gradient (before it is rounded)
+ * Any of the four outputs may be NULL, but not all of them; without drop, dx is dresidual and one of them is enough. */
+DWM_API dwm_status_t dwm_norm_join_backward(const dwm_norm_plan_t* plan, const dwm_dropout_t* drop, const void* dy_dev,
+                                            const void* dz_dev, const void* z_dev, const void* gamma_dev,
+                                            const float* mean_dev, const float* rstd_dev, void* dx_dev, void* dresidual_dev,
+                                            void* dgamma_dev, void* dbeta_dev, void* stream);
+
 DWM_API const char* dwm_status_string(dwm_status_t status);
 
 #ifdef __cplusplus

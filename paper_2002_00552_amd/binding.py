@@ -64,8 +64,23 @@ class dwm_bwd_filter_info_t(ctypes.Structure):
                 ("direct_flops", ctypes.c_double), ("winograd_flops", ctypes.c_double)]
 
 
+DWM_F32, DWM_F16, DWM_BF16 = range(3)
+
+
+class dwm_dropout_t(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_ulonglong), ("sequence", ctypes.c_ulonglong),
+                ("sequence_dev", ctypes.c_void_p)]
+
+
+class dwm_norm_info_t(ctypes.Structure):
+    _fields_ = [("outer", ctypes.c_longlong), ("C", ctypes.c_int), ("inner", ctypes.c_longlong),
+                ("forward_kernel", ctypes.c_int), ("backward_kernel", ctypes.c_int), ("splits", ctypes.c_int)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
+_L = ctypes.c_longlong
+_DROP = ctypes.POINTER(dwm_dropout_t)
 _SIGNATURES = {
     "dwm_plan_create": (_I, [ctypes.POINTER(_P)] + [_I] * 9),
     "dwm_plan_destroy": (_I, [_P]),
@@ -132,6 +147,18 @@ _SIGNATURES = {
     "dwm_bf16_conv_forward_f32out": (_I, [_P, _P, _P, _P, _P]),
     "dwm_bf16_input_transform": (_I, [_P, _P, _P]),
     "dwm_bf16_contract_output": (_I, [_P, _P, _P, _P]),
+    "dwm_dropout_forward": (_I, [_DROP, _I, _L, _P, _P, _P]),
+    "dwm_dropout_backward": (_I, [_DROP, _I, _L, _P, _P, _P]),
+    "dwm_norm_plan_create": (_I, [ctypes.POINTER(_P), _L, _I, _L, _I, _I, ctypes.c_double]),
+    "dwm_norm_plan_destroy": (_I, [_P]),
+    "dwm_norm_plan_info": (_I, [_P, ctypes.POINTER(dwm_norm_info_t)]),
+    "dwm_norm_set_stride": (_I, [_P, ctypes.c_char_p, _L]),
+    "dwm_norm_workspace_bytes": (ctypes.c_size_t, [_P]),
+    "dwm_norm_set_workspace": (_I, [_P, _P, ctypes.c_size_t]),
+    "dwm_norm_forward": (_I, [_P] * 8),
+    "dwm_norm_backward": (_I, [_P] * 10),
+    "dwm_norm_join_forward": (_I, [_P, _DROP] + [_P] * 9),
+    "dwm_norm_join_backward": (_I, [_P, _DROP] + [_P] * 11),
 }
 EXPORTS = sorted(_SIGNATURES)
 
@@ -449,3 +476,60 @@ def dwm_bf16_input_transform(plan, x_dev, stream=None):
 
 def dwm_bf16_contract_output(plan, U_dev, y_dev, stream=None):
     _check(lib().dwm_bf16_contract_output(plan, U_dev, y_dev, stream), "dwm_bf16_contract_output")
+
+
+def dwm_dropout_forward(drop, type, n, x_dev, y_dev, stream=None):
+    _check(lib().dwm_dropout_forward(drop, type, n, x_dev, y_dev, stream), "dwm_dropout_forward")
+
+
+def dwm_dropout_backward(drop, type, n, dy_dev, dx_dev, stream=None):
+    _check(lib().dwm_dropout_backward(drop, type, n, dy_dev, dx_dev, stream), "dwm_dropout_backward")
+
+
+def dwm_norm_plan_create(outer, C, inner, type, param_type, eps):
+    h = _P()
+    _check(lib().dwm_norm_plan_create(ctypes.byref(h), outer, C, inner, type, param_type, eps), "dwm_norm_plan_create")
+    return h
+
+
+def dwm_norm_plan_destroy(plan):
+    _check(lib().dwm_norm_plan_destroy(plan), "dwm_norm_plan_destroy")
+
+
+def dwm_norm_plan_info(plan):
+    info = dwm_norm_info_t()
+    _check(lib().dwm_norm_plan_info(plan, ctypes.byref(info)), "dwm_norm_plan_info")
+    return info
+
+
+def dwm_norm_set_stride(plan, tensor, stride):
+    _check(lib().dwm_norm_set_stride(plan, tensor.encode(), stride), "dwm_norm_set_stride(%s)" % tensor)
+
+
+def dwm_norm_workspace_bytes(plan):
+    return int(lib().dwm_norm_workspace_bytes(plan))
+
+
+def dwm_norm_set_workspace(plan, ws_dev, nbytes):
+    _check(lib().dwm_norm_set_workspace(plan, ws_dev, nbytes), "dwm_norm_set_workspace")
+
+
+def dwm_norm_forward(plan, x_dev, gamma_dev, beta_dev, y_dev, mean_dev=None, rstd_dev=None, stream=None):
+    _check(lib().dwm_norm_forward(plan, x_dev, gamma_dev, beta_dev, y_dev, mean_dev, rstd_dev, stream), "dwm_norm_forward")
+
+
+def dwm_norm_backward(plan, dy_dev, x_dev, gamma_dev, mean_dev, rstd_dev, dx_dev, dgamma_dev, dbeta_dev, stream=None):
+    _check(lib().dwm_norm_backward(plan, dy_dev, x_dev, gamma_dev, mean_dev, rstd_dev, dx_dev, dgamma_dev, dbeta_dev, stream),
+           "dwm_norm_backward")
+
+
+def dwm_norm_join_forward(plan, drop, x_dev, residual_dev, gamma_dev, beta_dev, z_dev, y_dev, mean_dev=None, rstd_dev=None,
+                          stream=None):
+    _check(lib().dwm_norm_join_forward(plan, drop, x_dev, residual_dev, gamma_dev, beta_dev, z_dev, y_dev, mean_dev, rstd_dev,
+                                       stream), "dwm_norm_join_forward")
+
+
+def dwm_norm_join_backward(plan, drop, dy_dev, dz_dev, z_dev, gamma_dev, mean_dev, rstd_dev, dx_dev, dresidual_dev, dgamma_dev,
+                           dbeta_dev, stream=None):
+    _check(lib().dwm_norm_join_backward(plan, drop, dy_dev, dz_dev, z_dev, gamma_dev, mean_dev, rstd_dev, dx_dev, dresidual_dev,
+                                        dgamma_dev, dbeta_dev, stream), "dwm_norm_join_backward")

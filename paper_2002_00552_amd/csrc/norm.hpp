@@ -1,0 +1,63 @@
+// Layer norms, dropouts and joins of residual branches: what the host side and the kernels share.  Plain C++.
+#pragma once
+#include <cstddef>
+#include <cstdint>
+
+#include "../../include/dwm.h"
+
+namespace dwm {
+
+// What a kernel needs of a dwm_dropout_t.
+struct DropArgs {
+    int mode;            // kDropNone, kDropDraw, kDropAll
+    uint32_t threshold;  // an element is kept where its word is not below this
+    float scale;         // 1 / (1 - p)
+    uint32_t seed_lo, seed_hi;
+    uint64_t sequence;
+    const unsigned long long* sequence_dev;  // added to sequence if not null
+};
+enum { kDropNone = 0, kDropDraw = 1, kDropAll = 2 };
+
+// Tensors [outer][C][inner]: element (o, c, i) lies at o * stride + c * inner + i.
+enum NormTensor { kNormX, kNormResidual, kNormZ, kNormY, kNormDy, kNormDz, kNormDx, kNormDresidual, kNormTensors };
+
+// One call.  The norm's input is z: the plain norm's x goes by that name in the backward kernels, and its dx by dresidual.
+struct NormArgs {
+    const void *x, *residual, *dy, *dz, *gamma, *beta;
+    void *z, *y, *dx, *dresidual, *dgamma, *dbeta;
+    float *mean, *rstd;  // [outer][inner]
+    float* partial;      // [splits][2][C]: sums of dy * xhat and of dy over a part of the positions
+    long long stride[kNormTensors];
+    long long outer, inner;
+    int C;
+    int param_typed;  // parameters have the tensors' type, otherwise binary32
+    int splits;
+    float eps;
+    DropArgs drop;
+};
+
+// How a plan's kernels are cut.
+struct NormShape {
+    int kernel;  // 0: norm_any.hip
+    int splits;  // of the parameters' gradients
+};
+
+constexpr int kNormMaxSplits = 256;
+
+NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, bool backward);
+
+dwm_status_t launch_norm_any_forward(const NormArgs& a, dwm_type_t type, bool join, void* stream);
+dwm_status_t launch_norm_any_backward(const NormArgs& a, dwm_type_t type, void* stream);
+dwm_status_t launch_dropout(const DropArgs& d, dwm_type_t type, long long n, const void* x, void* y, void* stream);
+
+}  // namespace dwm
+
+struct dwm_norm_plan {
+    long long outer, inner;
+    int C;
+    dwm_type_t type, param_type;
+    float eps;
+    long long stride[dwm::kNormTensors];
+    dwm::NormShape forward, backward;
+    void* ws;
+};

@@ -1,0 +1,231 @@
+// Layer norm over the channels of [outer][C][inner] and its gradients, with or without the join of a residual branch, for any
+// sizes (gfx950).  A position (o, i) is a norm of its own:
+//     m = (1/C) sum_c z,  v = (1/C) sum_c (z - m)^2,  r = 1 / sqrt(v + eps),  y = (z - m) r gamma_c + beta_c
+//     g = dy gamma,  dz = r (g - (1/C) sum_c g - xhat (1/C) sum_c g xhat),  dgamma_c = sum_{o,i} dy xhat,  dbeta_c = sum_{o,i} dy
+// with xhat = (z - m) r and, in a join, z = residual + dropout(x) rounded to its type.
+//
+// Nothing is held from one pass over the channels to the next, so a norm is read three times and its gradient twice; the kernels
+// that keep a norm in registers (norm_impl.inc) take every size that they can.  Sums are in binary32.  The second pass takes the
+// sums of d and of d^2, d = z - m: the first corrects the rounding of m, m + (1/C) sum d, and the variance with it.
+// A workgroup owns L positions next to each other, 256 / L threads each: lanes lie along what is contiguous, the channels of a
+// row (L = 1) or the pixels of a map (L = 64).  A thread meets the same elements in every pass, so z may be the residual's own
+// memory, and what a pass wrote is there for the next.
+#include "elem.hpp"
+#include "philox.hpp"
+
+namespace dwm {
+
+template <class T> __device__ __forceinline__ float param(const void* p, int typed, long long c, float none)
+{
+    if (!p) return none;
+    return typed ? (float)((const T*)p)[c] : ((const float*)p)[c];
+}
+
+// The sum over the 256 / L threads of a position, for all of them.
+template <int L>
+__device__ __forceinline__ float position_sum(float v, float* lds)
+{
+    const int tid = threadIdx.x;
+    __syncthreads();  // what was read last
+    lds[tid] = v;
+    __syncthreads();
+#pragma unroll
+    for (int h = 128; h >= L; h /= 2) {
+        if (tid < h) lds[tid] += lds[tid + h];
+        __syncthreads();
+    }
+    return lds[tid % L];
+}
+
+template <class T, int L, bool JOIN>
+__global__ __launch_bounds__(256) void norm_any_forward_kernel(NormArgs a)
+{
+    __shared__ float lds[256];
+    const int p = threadIdx.x % L, g = threadIdx.x / L;
+    constexpr int G = 256 / L;
+    const long long positions = a.outer * a.inner;
+    const uint64_t sequence = drop_sequence(a.drop);
+    const float inv_c = 1.0f / (float)a.C;
+    const T *x = (const T*)a.x, *residual = (const T*)a.residual;
+    T *z = (T*)a.z, *y = (T*)a.y;
+    for (long long t0 = (long long)blockIdx.x * L; t0 < positions; t0 += (long long)gridDim.x * L) {
+        const long long t = t0 + p;
+        const int n = t < positions ? a.C : 0;  // every thread meets the barriers
+        const long long o = t / a.inner, i = t % a.inner;
+        const T* xp = x + o * a.stride[kNormX] + i;
+        const T* rp = residual + o * a.stride[kNormResidual] + i;
+        T* zp = z + o * a.stride[kNormZ] + i;
+        float sum = 0.0f;
+        for (int c = g; c < n; c += G) {
+            float v = (float)xp[c * a.inner];
+            if (JOIN) {
+                bool keep[1] = {a.drop.mode == kDropNone};
+                if (a.drop.mode == kDropDraw) drop_draw<1, false>(a.drop, sequence, (uint64_t)((o * a.C + c) * a.inner + i), keep);
+                const T r = (T)join_sum((float)rp[c * a.inner], drop_scaled(v, keep[0], a.drop.scale));
+                zp[c * a.inner] = r;
+                v = (float)r;
+            }
+            sum += v;
+        }
+        const T* vp = JOIN ? zp : xp;
+        const float m0 = position_sum<L>(sum, lds) * inv_c;
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int c = g; c < n; c += G) {
+            const float d = (float)vp[c * a.inner] - m0;
+            s1 += d;
+            s2 += d * d;
+        }
+        s1 = position_sum<L>(s1, lds) * inv_c;
+        s2 = position_sum<L>(s2, lds) * inv_c;
+        const float var = s2 - s1 * s1;
+        const float rstd = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + a.eps);  // (NaN stays)
+        T* yp = y + o * a.stride[kNormY] + i;
+        for (int c = g; c < n; c += G) {
+            const float d = (float)vp[c * a.inner] - m0 - s1;
+            yp[c * a.inner] = (T)(d * rstd * param<T>(a.gamma, a.param_typed, c, 1.0f) + param<T>(a.beta, a.param_typed, c, 0.0f));
+        }
+        if (g == 0 && n) {
+            if (a.mean) a.mean[t] = m0 + s1;
+            if (a.rstd) a.rstd[t] = rstd;
+        }
+    }
+}
+
+template <class T, int L>
+__global__ __launch_bounds__(256) void norm_any_backward_kernel(NormArgs a)
+{
+    __shared__ float lds[256];
+    const int p = threadIdx.x % L, g = threadIdx.x / L;
+    constexpr int G = 256 / L;
+    const long long positions = a.outer * a.inner;
+    const uint64_t sequence = drop_sequence(a.drop);
+    const float inv_c = 1.0f / (float)a.C;
+    for (long long t0 = (long long)blockIdx.x * L; t0 < positions; t0 += (long long)gridDim.x * L) {
+        const long long t = t0 + p;
+        const int n = t < positions ? a.C : 0;
+        const long long o = t / a.inner, i = t % a.inner;
+        const float mean = n ? a.mean[t] : 0.0f, rstd = n ? a.rstd[t] : 0.0f;
+        const T* dyp = (const T*)a.dy + o * a.stride[kNormDy] + i;
+        const T* zp = (const T*)a.z + o * a.stride[kNormZ] + i;
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int c = g; c < n; c += G) {
+            const float gr = (float)dyp[c * a.inner] * param<T>(a.gamma, a.param_typed, c, 1.0f);
+            s1 += gr;
+            s2 += gr * (((float)zp[c * a.inner] - mean) * rstd);
+        }
+        s1 = position_sum<L>(s1, lds) * inv_c;
+        s2 = position_sum<L>(s2, lds) * inv_c;
+        for (int c = g; c < n; c += G) {
+            const long long at = c * a.inner;
+            const float gr = (float)dyp[at] * param<T>(a.gamma, a.param_typed, c, 1.0f);
+            const float xhat = ((float)zp[at] - mean) * rstd;
+            float d = rstd * (gr - s1 - xhat * s2);
+            if (a.dz) d += (float)((const T*)a.dz)[o * a.stride[kNormDz] + i + at];
+            if (a.dresidual) ((T*)a.dresidual)[o * a.stride[kNormDresidual] + i + at] = (T)d;
+            if (a.dx) {
+                bool keep[1] = {a.drop.mode == kDropNone};
+                if (a.drop.mode == kDropDraw) drop_draw<1, false>(a.drop, sequence, (uint64_t)((o * a.C + c) * a.inner + i), keep);
+                ((T*)a.dx)[o * a.stride[kNormDx] + i + at] = (T)drop_scaled(d, keep[0], a.drop.scale);
+            }
+        }
+    }
+}
+
+// The parameters' gradients over one split of the positions: L channels of a workgroup, 256 / L threads each.
+template <class T, int L>
+__global__ __launch_bounds__(256) void norm_any_params_kernel(NormArgs a)
+{
+    __shared__ float lds[256];
+    const int c = blockIdx.x * L + threadIdx.x % L;
+    const long long positions = a.outer * a.inner;
+    float dgamma = 0.0f, dbeta = 0.0f;
+    if (c < a.C)
+        for (long long t = (long long)blockIdx.y * (256 / L) + threadIdx.x / L; t < positions; t += (long long)gridDim.y * (256 / L)) {
+            const long long o = t / a.inner, i = t % a.inner;
+            const float dy = (float)((const T*)a.dy)[o * a.stride[kNormDy] + c * a.inner + i];
+            const float z = (float)((const T*)a.z)[o * a.stride[kNormZ] + c * a.inner + i];
+            dgamma += dy * ((z - a.mean[t]) * a.rstd[t]);
+            dbeta += dy;
+        }
+    dgamma = position_sum<L>(dgamma, lds);
+    dbeta = position_sum<L>(dbeta, lds);
+    if (threadIdx.x < L && c < a.C) {
+        a.partial[(long long)blockIdx.y * 2 * a.C + c] = dgamma;
+        a.partial[((long long)blockIdx.y * 2 + 1) * a.C + c] = dbeta;
+    }
+}
+
+// The splits' sums added up, in an order that does not vary: 64 channels of a workgroup, four threads each.
+template <class T>
+__global__ __launch_bounds__(256) void norm_params_final_kernel(NormArgs a)
+{
+    __shared__ float lds[256];
+    const int c = blockIdx.x * 64 + threadIdx.x % 64, which = blockIdx.y;
+    float sum = 0.0f;
+    if (c < a.C)
+        for (int s = threadIdx.x / 64; s < a.splits; s += 4) sum += a.partial[((long long)s * 2 + which) * a.C + c];
+    sum = position_sum<64>(sum, lds);
+    void* out = which ? a.dbeta : a.dgamma;
+    if (threadIdx.x < 64 && c < a.C && out) {
+        if (a.param_typed) ((T*)out)[c] = (T)sum;
+        else ((float*)out)[c] = sum;
+    }
+}
+
+template <class T, int L>
+static dwm_status_t forward(const NormArgs& a, bool join, hipStream_t stream)
+{
+    const long long tiles = (a.outer * a.inner + L - 1) / L;
+    const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20));
+    if (join) hipLaunchKernelGGL((norm_any_forward_kernel<T, L, true>), grid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((norm_any_forward_kernel<T, L, false>), grid, dim3(256), 0, stream, a);
+    return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
+}
+
+template <class T>
+static dwm_status_t backward(const NormArgs& a, hipStream_t stream)
+{
+    const long long positions = a.outer * a.inner;
+    if (a.dgamma || a.dbeta) {  // first: dx may be dy's own memory
+        if (a.inner == 1)
+            hipLaunchKernelGGL((norm_any_params_kernel<T, 64>), dim3((a.C + 63) / 64, a.splits), dim3(256), 0, stream, a);
+        else
+            hipLaunchKernelGGL((norm_any_params_kernel<T, 1>), dim3(a.C, a.splits), dim3(256), 0, stream, a);
+        if (hipGetLastError() != hipSuccess) return DWM_ERR_HIP;
+        hipLaunchKernelGGL((norm_params_final_kernel<T>), dim3((a.C + 63) / 64, 2), dim3(256), 0, stream, a);
+        if (hipGetLastError() != hipSuccess) return DWM_ERR_HIP;
+    }
+    if ((a.dx || a.dresidual) && positions > 0) {
+        const int L = a.inner == 1 ? 1 : 64;
+        const long long tiles = (positions + L - 1) / L;
+        const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20));
+        if (L == 1) hipLaunchKernelGGL((norm_any_backward_kernel<T, 1>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((norm_any_backward_kernel<T, 64>), grid, dim3(256), 0, stream, a);
+        if (hipGetLastError() != hipSuccess) return DWM_ERR_HIP;
+    }
+    return DWM_OK;
+}
+
+dwm_status_t launch_norm_any_forward(const NormArgs& a, dwm_type_t type, bool join, void* stream)
+{
+    const hipStream_t s = (hipStream_t)stream;
+    if (a.outer == 0) return DWM_OK;
+    switch (type) {
+        case DWM_F32: return a.inner == 1 ? forward<float, 1>(a, join, s) : forward<float, 64>(a, join, s);
+        case DWM_F16: return a.inner == 1 ? forward<_Float16, 1>(a, join, s) : forward<_Float16, 64>(a, join, s);
+        case DWM_BF16: return a.inner == 1 ? forward<__bf16, 1>(a, join, s) : forward<__bf16, 64>(a, join, s);
+    }
+    return DWM_ERR_INVALID_ARG;
+}
+
+dwm_status_t launch_norm_any_backward(const NormArgs& a, dwm_type_t type, void* stream)
+{
+    switch (type) {
+        case DWM_F32: return backward<float>(a, (hipStream_t)stream);
+        case DWM_F16: return backward<_Float16>(a, (hipStream_t)stream);
+        case DWM_BF16: return backward<__bf16>(a, (hipStream_t)stream);
+    }
+    return DWM_ERR_INVALID_ARG;
+}
+
+}  // namespace dwm
