@@ -491,7 +491,7 @@ typedef struct {
     long long outer;
     int C;
     long long inner;
-    int forward_kernel, backward_kernel; /* 0: the kernels for any size */
+    int forward_kernel, backward_kernel; /* dwm_norm_set_variant's numbers */
     int splits;                          /* parts of the positions whose sums of the parameters' gradients are added up last */
 } dwm_norm_info_t;
 
@@ -504,6 +504,11 @@ DWM_API dwm_status_t dwm_norm_plan_info(const dwm_norm_plan_t* plan, dwm_norm_in
 /* Elements between one o and the next of a tensor ("x", "residual", "z", "y", "dy", "dz", "dx", "dresidual"): at least C*inner,
  * which is the default; more where a tensor is a slice of a wider one.  May be called at any time. */
 DWM_API dwm_status_t dwm_norm_set_stride(dwm_norm_plan_t* plan, const char* tensor, long long stride);
+/* A kernel by number, for tuning and tests: stage "forward" or "backward" (this one before dwm_norm_set_workspace only,
+ * DWM_ERR_WORKSPACE afterwards); 0 = the kernels for any size; rows (inner = 1): 1 .. 12, the library's internal table of threads of a row
+ * and vectors of a thread; maps: 100 .. 104 with sixteen bytes of pixels a lane, 200 .. 204 with one; negative: the planner's
+ * choice.  DWM_ERR_INVALID_ARG for one that cannot hold C channels.  All give the same results up to the order of sums. */
+DWM_API dwm_status_t dwm_norm_set_variant(dwm_norm_plan_t* plan, const char* stage, int variant);
 /* The workspace holds partial sums of dgamma and dbeta: 256-byte aligned, needed by backward calls that are asked for one of
  * them and by no other call. */
 DWM_API size_t dwm_norm_workspace_bytes(const dwm_norm_plan_t* plan);

@@ -153,6 +153,7 @@ _SIGNATURES = {
     "dwm_norm_plan_destroy": (_I, [_P]),
     "dwm_norm_plan_info": (_I, [_P, ctypes.POINTER(dwm_norm_info_t)]),
     "dwm_norm_set_stride": (_I, [_P, ctypes.c_char_p, _L]),
+    "dwm_norm_set_variant": (_I, [_P, ctypes.c_char_p, _I]),
     "dwm_norm_workspace_bytes": (ctypes.c_size_t, [_P]),
     "dwm_norm_set_workspace": (_I, [_P, _P, ctypes.c_size_t]),
     "dwm_norm_forward": (_I, [_P] * 8),
@@ -504,6 +505,10 @@ def dwm_norm_plan_info(plan):
 
 def dwm_norm_set_stride(plan, tensor, stride):
     _check(lib().dwm_norm_set_stride(plan, tensor.encode(), stride), "dwm_norm_set_stride(%s)" % tensor)
+
+
+def dwm_norm_set_variant(plan, stage, variant):
+    _check(lib().dwm_norm_set_variant(plan, stage.encode(), variant), "dwm_norm_set_variant(%s)" % stage)
 
 
 def dwm_norm_workspace_bytes(plan):

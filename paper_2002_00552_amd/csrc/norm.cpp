@@ -8,16 +8,43 @@
 
 namespace dwm {
 
-// Splits of the positions for the parameters' gradients: enough for the chip, none without some work.
-NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t, bool)
+static NormShape any_shape(long long positions, int C, bool rows)
 {
-    const long long positions = outer * inner;
-    NormShape s{};
-    const long long groups = inner == 1 ? (C + 63) / 64 : C, threads = inner == 1 ? 4 : 256;
+    const long long groups = rows ? (C + 63) / 64 : C, threads = rows ? 4 : 256;
     long long splits = (positions + 16 * threads - 1) / (16 * threads);
     if (splits * groups > 4096) splits = 4096 / groups;
-    s.splits = (int)(splits < 1 ? 1 : splits > kNormMaxSplits ? kNormMaxSplits : splits);
-    return s;
+    return {kNormAny, (int)(splits < 1 ? 1 : splits > 256 ? 256 : splits)};
+}
+
+static long long at_most(long long v, long long most) { return v < most ? v : most; }
+
+NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, bool backward, int variant)
+{
+    const long long positions = outer * inner;
+    const int vec = type == DWM_F32 ? 4 : 8;
+    const NormShape any = any_shape(positions, C, inner == 1), none{-1, 0};
+    if (variant == kNormAny || (variant < 0 && positions == 0)) return any;
+    if (inner == 1) {
+        int shape = variant - kNormRowsFirst;
+        if (variant < 0)
+            for (shape = 0; shape < kNormRowsShapes && kNormRows[shape].tpr * kNormRows[shape].k * vec < C;) ++shape;
+        const bool ok = shape >= 0 && shape < kNormRowsShapes && kNormRows[shape].tpr * kNormRows[shape].k * vec >= C && C >= vec;
+        if (!ok) return variant < 0 ? any : none;
+        const int tpr = kNormRows[shape].tpr, smallest = backward ? kNormRowsBackwardThreads : 256;
+        const int rows = (tpr > smallest ? tpr : smallest) / tpr;
+        const long long blocks = (outer + rows - 1) / rows;
+        return {kNormRowsFirst + shape, (int)at_most(blocks, backward ? 512 : 2048)};
+    }
+    bool one = variant < 0 ? inner < vec : variant >= kNormMapsOne;
+    int shape = variant - (one ? kNormMapsOne : kNormMapsVec);
+    if (variant < 0)
+        for (shape = 0; shape < kNormMapsShapes && kNormMaps[shape].cg * kNormMaps[shape].k < C;) ++shape;
+    const long long vectors = one ? positions : outer * ((inner + vec - 1) / vec), limit = (1LL << 31) - 1;
+    const bool ok = shape >= 0 && shape < kNormMapsShapes && kNormMaps[shape].cg * kNormMaps[shape].k >= C && (one || inner >= vec) &&
+                    vectors < limit && inner < limit;
+    if (!ok) return variant < 0 ? any : none;
+    const long long tiles = (vectors + kNormMaps[shape].pl - 1) / kNormMaps[shape].pl;
+    return {(one ? kNormMapsOne : kNormMapsVec) + shape, (int)at_most(tiles, backward ? 512 : 4096)};
 }
 
 static const char* const kTensorNames[kNormTensors] = {"x", "residual", "z", "y", "dy", "dz", "dx", "dresidual"};
@@ -54,7 +81,7 @@ static NormArgs args_of(const dwm_norm_plan& p, const NormShape& shape)
     a.inner = p.inner;
     a.C = p.C;
     a.param_typed = p.param_type == p.type && p.type != DWM_F32;
-    a.splits = shape.splits;
+    a.splits = shape.blocks;
     a.eps = p.eps;
     a.partial = (float*)p.ws;
     a.drop.scale = 1.0f;
@@ -83,15 +110,29 @@ static bool params_ok(const dwm_norm_plan& p, std::initializer_list<const void*>
 }
 static bool stats_ok(const void* mean, const void* rstd) { return aligned(mean, 4) && aligned(rstd, 4); }
 
+static dwm_status_t run_kernel(const dwm_norm_plan& p, const NormArgs& a, const NormShape& shape, bool backward, bool join, void* stream)
+{
+    switch (p.type) {
+        case DWM_F32: return launch_norm_f32(a, shape, backward, join, stream);
+        case DWM_F16: return launch_norm_f16(a, shape, backward, join, stream);
+        case DWM_BF16: return launch_norm_bf16(a, shape, backward, join, stream);
+    }
+    return DWM_ERR_INVALID_ARG;
+}
+
 static dwm_status_t run_forward(const dwm_norm_plan& p, const NormArgs& a, bool join, void* stream)
 {
-    return launch_norm_any_forward(a, p.type, join, stream);
+    if (p.outer == 0) return DWM_OK;
+    return p.forward.kernel == kNormAny ? launch_norm_any_forward(a, p.type, join, stream) : run_kernel(p, a, p.forward, false, join, stream);
 }
 
 static dwm_status_t run_backward(const dwm_norm_plan& p, const NormArgs& a, void* stream)
 {
-    if ((a.dgamma || a.dbeta) && !p.ws) return DWM_ERR_WORKSPACE;
-    return launch_norm_any_backward(a, p.type, stream);
+    const bool params = a.dgamma || a.dbeta;
+    if (params && !p.ws) return DWM_ERR_WORKSPACE;
+    if (p.backward.kernel == kNormAny) return launch_norm_any_backward(a, p.type, stream);
+    const dwm_status_t st = run_kernel(p, a, p.backward, true, false, stream);
+    return st != DWM_OK || !params ? st : launch_norm_params_final(a, p.type, stream);
 }
 
 }  // namespace dwm
@@ -116,8 +157,8 @@ dwm_status_t dwm_norm_plan_create(dwm_norm_plan_t** out, long long outer, int C,
     p->param_type = param_type;
     p->eps = (float)eps;
     for (long long& s : p->stride) s = C * inner;
-    p->forward = norm_choose(outer, C, inner, type, false);
-    p->backward = norm_choose(outer, C, inner, type, true);
+    p->forward = norm_choose(outer, C, inner, type, false, -1);
+    p->backward = norm_choose(outer, C, inner, type, true, -1);
     *out = p;
     return DWM_OK;
 }
@@ -141,6 +182,19 @@ dwm_status_t dwm_norm_set_stride(dwm_norm_plan_t* plan, const char* tensor, long
     return DWM_OK;
 }
 
+dwm_status_t dwm_norm_set_variant(dwm_norm_plan_t* plan, const char* stage, int variant)
+{
+    using namespace dwm;
+    if (!plan || !stage) return DWM_ERR_INVALID_ARG;
+    const bool backward = !std::strcmp(stage, "backward");
+    if (!backward && std::strcmp(stage, "forward")) return DWM_ERR_INVALID_ARG;
+    if (backward && plan->ws) return DWM_ERR_WORKSPACE;
+    const NormShape s = norm_choose(plan->outer, plan->C, plan->inner, plan->type, backward, variant);
+    if (s.kernel < 0) return DWM_ERR_INVALID_ARG;
+    (backward ? plan->backward : plan->forward) = s;
+    return DWM_OK;
+}
+
 dwm_status_t dwm_norm_plan_info(const dwm_norm_plan_t* plan, dwm_norm_info_t* info)
 {
     if (!plan || !info) return DWM_ERR_INVALID_ARG;
@@ -149,13 +203,13 @@ dwm_status_t dwm_norm_plan_info(const dwm_norm_plan_t* plan, dwm_norm_info_t* in
     info->inner = plan->inner;
     info->forward_kernel = plan->forward.kernel;
     info->backward_kernel = plan->backward.kernel;
-    info->splits = plan->backward.splits;
+    info->splits = plan->backward.blocks;
     return DWM_OK;
 }
 
 size_t dwm_norm_workspace_bytes(const dwm_norm_plan_t* plan)
 {
-    return plan ? (size_t)plan->backward.splits * 2 * plan->C * sizeof(float) : 0;
+    return plan ? (size_t)plan->backward.blocks * 2 * plan->C * sizeof(float) : 0;
 }
 
 dwm_status_t dwm_norm_set_workspace(dwm_norm_plan_t* plan, void* ws_dev, size_t bytes)

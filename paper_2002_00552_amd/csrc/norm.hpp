@@ -36,18 +36,38 @@ struct NormArgs {
     DropArgs drop;
 };
 
-// How a plan's kernels are cut.
+// The shapes that the register-resident kernels (norm_impl.inc) are built in.  Rows: threads of a row, vectors of sixteen bytes of a
+// thread.  Maps: lanes along the pixels, groups along the channels, channels of a thread.
+struct NormRows {
+    int tpr, k;
+};
+struct NormMaps {
+    int pl, cg, k;
+};
+constexpr NormRows kNormRows[] = {{8, 1}, {16, 1}, {32, 1}, {64, 1}, {64, 2}, {64, 4}, {256, 1}, {256, 2}, {256, 4}, {1024, 1}, {1024, 2}, {1024, 4}};
+constexpr NormMaps kNormMaps[] = {{64, 4, 8}, {16, 16, 8}, {16, 32, 8}, {16, 64, 8}, {16, 64, 16}};
+constexpr int kNormRowsShapes = sizeof(kNormRows) / sizeof(kNormRows[0]), kNormMapsShapes = sizeof(kNormMaps) / sizeof(kNormMaps[0]);
+constexpr int kNormRowsBackwardThreads = 512;
+
+// A plan's kernel: 0 (norm_any.hip), or a shape from here on of rows, of maps with sixteen bytes of pixels a lane, with one pixel a lane.
+constexpr int kNormAny = 0, kNormRowsFirst = 1, kNormMapsVec = 100, kNormMapsOne = 200;
+
 struct NormShape {
-    int kernel;  // 0: norm_any.hip
-    int splits;  // of the parameters' gradients
+    int kernel;
+    int blocks;  // workgroups; backward: splits of the parameters' gradients too
 };
 
-constexpr int kNormMaxSplits = 256;
+constexpr int kNormMaxSplits = 1024;
 
-NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, bool backward);
+// The planner's choice (variant < 0), or the kernel asked for; kernel = -1: it does not apply.
+NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, bool backward, int variant);
 
 dwm_status_t launch_norm_any_forward(const NormArgs& a, dwm_type_t type, bool join, void* stream);
 dwm_status_t launch_norm_any_backward(const NormArgs& a, dwm_type_t type, void* stream);
+dwm_status_t launch_norm_params_final(const NormArgs& a, dwm_type_t type, void* stream);
+dwm_status_t launch_norm_f32(const NormArgs& a, const NormShape& shape, bool backward, bool join, void* stream);
+dwm_status_t launch_norm_f16(const NormArgs& a, const NormShape& shape, bool backward, bool join, void* stream);
+dwm_status_t launch_norm_bf16(const NormArgs& a, const NormShape& shape, bool backward, bool join, void* stream);
 dwm_status_t launch_dropout(const DropArgs& d, dwm_type_t type, long long n, const void* x, void* y, void* stream);
 
 }  // namespace dwm

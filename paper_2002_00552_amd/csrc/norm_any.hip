@@ -6,20 +6,13 @@
 //
 // Nothing is held from one pass over the channels to the next, so a norm is read three times and its gradient twice; the kernels
 // that keep a norm in registers (norm_impl.inc) take every size that they can.  Sums are in binary32.  The second pass takes the
-// sums of d and of d^2, d = z - m: the first corrects the rounding of m, m + (1/C) sum d, and the variance with it.
+// sums of d and of d^2, d = z - m; the first of them tells how far m was off (norm_device.hpp).
 // A workgroup owns L positions next to each other, 256 / L threads each: lanes lie along what is contiguous, the channels of a
 // row (L = 1) or the pixels of a map (L = 64).  A thread meets the same elements in every pass, so z may be the residual's own
 // memory, and what a pass wrote is there for the next.
-#include "elem.hpp"
-#include "philox.hpp"
+#include "norm_device.hpp"
 
 namespace dwm {
-
-template <class T> __device__ __forceinline__ float param(const void* p, int typed, long long c, float none)
-{
-    if (!p) return none;
-    return typed ? (float)((const T*)p)[c] : ((const float*)p)[c];
-}
 
 // The sum over the 256 / L threads of a position, for all of them.
 template <int L>
@@ -77,16 +70,15 @@ __global__ __launch_bounds__(256) void norm_any_forward_kernel(NormArgs a)
         }
         s1 = position_sum<L>(s1, lds) * inv_c;
         s2 = position_sum<L>(s2, lds) * inv_c;
-        const float var = s2 - s1 * s1;
-        const float rstd = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + a.eps);  // (NaN stays)
+        const NormStats st = norm_stats(m0, s1, s2, a.eps);
         T* yp = y + o * a.stride[kNormY] + i;
         for (int c = g; c < n; c += G) {
-            const float d = (float)vp[c * a.inner] - m0 - s1;
-            yp[c * a.inner] = (T)(d * rstd * param<T>(a.gamma, a.param_typed, c, 1.0f) + param<T>(a.beta, a.param_typed, c, 0.0f));
+            const float d = (float)vp[c * a.inner] - m0 - st.off;
+            yp[c * a.inner] = (T)(d * st.rstd * param<T>(a.gamma, a.param_typed, c, 1.0f) + param<T>(a.beta, a.param_typed, c, 0.0f));
         }
         if (g == 0 && n) {
-            if (a.mean) a.mean[t] = m0 + s1;
-            if (a.rstd) a.rstd[t] = rstd;
+            if (a.mean) a.mean[t] = st.mean;
+            if (a.rstd) a.rstd[t] = st.rstd;
         }
     }
 }
@@ -155,21 +147,32 @@ __global__ __launch_bounds__(256) void norm_any_params_kernel(NormArgs a)
     }
 }
 
-// The splits' sums added up, in an order that does not vary: 64 channels of a workgroup, four threads each.
+// The splits' sums added up, in an order that does not vary: 32 channels of a workgroup, 32 threads each.
 template <class T>
-__global__ __launch_bounds__(256) void norm_params_final_kernel(NormArgs a)
+__global__ __launch_bounds__(1024) void norm_params_final_kernel(NormArgs a)
 {
-    __shared__ float lds[256];
-    const int c = blockIdx.x * 64 + threadIdx.x % 64, which = blockIdx.y;
+    __shared__ float lds[32][33];
+    const int lane = threadIdx.x % 32, group = threadIdx.x / 32, which = blockIdx.y;
+    const int c = blockIdx.x * 32 + lane;
     float sum = 0.0f;
     if (c < a.C)
-        for (int s = threadIdx.x / 64; s < a.splits; s += 4) sum += a.partial[((long long)s * 2 + which) * a.C + c];
-    sum = position_sum<64>(sum, lds);
+        for (int s = group; s < a.splits; s += 32) sum += a.partial[((long long)s * 2 + which) * a.C + c];
+    lds[group][lane] = sum;
+    __syncthreads();
+    sum = lanes_sum<32>(lds[lane][group]);  // a channel's 32 threads side by side
+    const int mine = blockIdx.x * 32 + group;
     void* out = which ? a.dbeta : a.dgamma;
-    if (threadIdx.x < 64 && c < a.C && out) {
-        if (a.param_typed) ((T*)out)[c] = (T)sum;
-        else ((float*)out)[c] = sum;
+    if (lane == 0 && mine < a.C && out) {
+        if (a.param_typed) ((T*)out)[mine] = (T)sum;
+        else ((float*)out)[mine] = sum;
     }
+}
+
+template <class T>
+static dwm_status_t params_final(const NormArgs& a, hipStream_t stream)
+{
+    hipLaunchKernelGGL((norm_params_final_kernel<T>), dim3((a.C + 31) / 32, 2), dim3(1024), 0, stream, a);
+    return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
 }
 
 template <class T, int L>
@@ -192,8 +195,8 @@ static dwm_status_t backward(const NormArgs& a, hipStream_t stream)
         else
             hipLaunchKernelGGL((norm_any_params_kernel<T, 1>), dim3(a.C, a.splits), dim3(256), 0, stream, a);
         if (hipGetLastError() != hipSuccess) return DWM_ERR_HIP;
-        hipLaunchKernelGGL((norm_params_final_kernel<T>), dim3((a.C + 63) / 64, 2), dim3(256), 0, stream, a);
-        if (hipGetLastError() != hipSuccess) return DWM_ERR_HIP;
+        const dwm_status_t st = params_final<T>(a, stream);
+        if (st != DWM_OK) return st;
     }
     if ((a.dx || a.dresidual) && positions > 0) {
         const int L = a.inner == 1 ? 1 : 64;
@@ -224,6 +227,16 @@ dwm_status_t launch_norm_any_backward(const NormArgs& a, dwm_type_t type, void* 
         case DWM_F32: return backward<float>(a, (hipStream_t)stream);
         case DWM_F16: return backward<_Float16>(a, (hipStream_t)stream);
         case DWM_BF16: return backward<__bf16>(a, (hipStream_t)stream);
+    }
+    return DWM_ERR_INVALID_ARG;
+}
+
+dwm_status_t launch_norm_params_final(const NormArgs& a, dwm_type_t type, void* stream)
+{
+    switch (type) {
+        case DWM_F32: return params_final<float>(a, (hipStream_t)stream);
+        case DWM_F16: return params_final<_Float16>(a, (hipStream_t)stream);
+        case DWM_BF16: return params_final<__bf16>(a, (hipStream_t)stream);
     }
     return DWM_ERR_INVALID_ARG;
 }

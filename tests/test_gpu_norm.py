@@ -456,3 +456,33 @@ def test_offsets_beyond_32_bits(shape):
     finally:
         torch.cuda.synchronize()
         dwm.dwm_norm_plan_destroy(plan)
+
+
+VARIANTS = [(shape, v) for shape, vs in (((70, 40, 1), range(1, 13)), ((9, 61, 1), range(1, 13)), ((5, 1000, 1), range(5, 13)), ((3, 16381, 1), range(12, 13)),
+                                         ((6, 32, 49), (100, 101, 102, 103, 104, 200, 201, 202, 203, 204)), ((3, 100, 18), (101, 102, 103, 104, 201, 204)),
+                                         ((2, 700, 270), (104, 204)), ((7, 90, 6), (201, 202, 203, 204)))
+            for v in (0, *vs)]
+
+
+@pytest.mark.parametrize("shape, variant", VARIANTS, ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else str(s))
+def test_every_kernel(shape, variant, monkeypatch):
+    """Each kernel that can hold the channels, asked for by number, in training and in a join."""
+    create = dwm.dwm_norm_plan_create
+
+    def asked(*args):
+        plan = create(*args)
+        dwm.dwm_norm_set_variant(plan, "forward", variant)
+        dwm.dwm_norm_set_variant(plan, "backward", variant)
+        info = dwm.dwm_norm_plan_info(plan)
+        assert (info.forward_kernel, info.backward_kernel) == (variant, variant)
+        return plan
+
+    monkeypatch.setattr(dwm, "dwm_norm_plan_create", asked)
+    for dtype in ("f32", "bf16", "f16"):
+        vec = 4 if dtype == "f32" else 8
+        if 100 <= variant < 200 and shape[2] < vec:
+            continue
+        if dtype == "f32" and 0 < variant < 13 and shape[1] > (32, 64, 128, 256, 512, 1024, 1024, 2048, 4096, 4096, 8192, 16384)[variant - 1]:
+            continue
+        check(shape, dtype, "f32", kind="offset")
+        check(shape, dtype, dtype, join=True, p=0.2, wide=5)

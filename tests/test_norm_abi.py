@@ -134,3 +134,23 @@ def test_dropouts_that_are_refused():
         _refused(dwm.DWM_ERR_INVALID_ARG, dwm.dwm_dropout_backward, *args)
     _refused(dwm.DWM_ERR_UNSUPPORTED, dwm.dwm_dropout_forward, drop, dwm.DWM_F32, (1 << 40) + 1, ONE, ONE)
     dwm.dwm_dropout_forward(drop, dwm.DWM_F32, 0, None, None)  # nothing to do
+
+
+def test_variants_that_do_not_apply():
+    rows, maps = dwm.dwm_norm_plan_create(8, 600, 1, dwm.DWM_F32, dwm.DWM_F32, 1e-5), dwm.dwm_norm_plan_create(8, 600, 7, dwm.DWM_BF16, dwm.DWM_F32, 1e-5)
+    try:
+        for plan, good, bad in ((rows, (0, 6, 12, -1), (1, 5, 13, 100, 204, 99)), (maps, (0, 204, -1), (1, 104, 203, 205, 300, 100))):
+            for stage in ("forward", "backward"):
+                for v in good:
+                    dwm.dwm_norm_set_variant(plan, stage, v)
+                for v in bad:
+                    _refused(dwm.DWM_ERR_INVALID_ARG, dwm.dwm_norm_set_variant, plan, stage, v)
+            _refused(dwm.DWM_ERR_INVALID_ARG, dwm.dwm_norm_set_variant, plan, "both", 0)
+            assert dwm.lib().dwm_norm_set_variant(plan, None, 0) == dwm.DWM_ERR_INVALID_ARG
+            dwm.dwm_norm_set_workspace(plan, ONE, 1 << 30)
+            dwm.dwm_norm_set_variant(plan, "forward", 0)
+            _refused(dwm.DWM_ERR_WORKSPACE, dwm.dwm_norm_set_variant, plan, "backward", 0)
+        assert dwm.lib().dwm_norm_set_variant(None, b"forward", 0) == dwm.DWM_ERR_INVALID_ARG
+    finally:
+        dwm.dwm_norm_plan_destroy(rows)
+        dwm.dwm_norm_plan_destroy(maps)
