@@ -16,7 +16,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropArgs d, long long firs
     const uint64_t sequence = drop_sequence(d);
     bool keep[V];
     if (e0 + V <= n) {
-        const uint4v r = load16(x + e0);
+        const uint4v r = load_vector<T, V>(x + e0);
         if (d.mode == kDropDraw) {
             drop_draw<V, true>(d, sequence, (uint64_t)e0, keep);
         } else {
@@ -24,10 +24,10 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropArgs d, long long firs
             for (int j = 0; j < V; ++j) keep[j] = d.mode == kDropNone;
         }
         float f[V];
-        unpack<T>(r, f);
+        unpack<T, V>(r, f);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = drop_scaled(f[j], keep[j], d.scale);
-        store16(y + e0, pack<T>(f));
+        store_vector<T, V>(y + e0, pack<T, V>(f));
     } else {
         drop_draw<V, true>(d, sequence, (uint64_t)e0, keep);
         for (int j = 0; j < V; ++j)

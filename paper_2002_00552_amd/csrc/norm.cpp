@@ -8,43 +8,82 @@
 
 namespace dwm {
 
+static long long at_most(long long v, long long most) { return v < most ? v : most; }
+
+// norm_any.hip: splits of the positions for the parameters' gradients, enough for the chip, none without some work.
 static NormShape any_shape(long long positions, int C, bool rows)
 {
     const long long groups = rows ? (C + 63) / 64 : C, threads = rows ? 4 : 256;
     long long splits = (positions + 16 * threads - 1) / (16 * threads);
     if (splits * groups > 4096) splits = 4096 / groups;
-    return {kNormAny, (int)(splits < 1 ? 1 : splits > 256 ? 256 : splits)};
+    return {kNormAny, (int)(splits < 1 ? 1 : at_most(splits, 256)), false};
 }
 
-static long long at_most(long long v, long long most) { return v < most ? v : most; }
+// Whether a shape can hold the norms of a plan.
+static bool rows_fit(int shape, int C, int vec, bool backward)
+{
+    if (shape < 0 || shape >= kNormRowsShapes) return false;
+    const NormRows& r = kNormRows[shape];
+    const int holds = r.tpr * r.k * vec;
+    return holds >= C && C >= vec && (backward ? r.backward && holds <= kNormRowsWidest : r.forward);
+}
+static bool maps_fit(int shape, int C, bool one)
+{
+    return shape >= 0 && shape < kNormMapsShapes && kNormMaps[shape].cg * kNormMaps[shape].k >= C && (!one || kNormMaps[shape].one);
+}
+
+// Rows, forward: the narrowest shape; below 2048 rows those with one vector a thread, a shorter way from the first load to the last store
+// (2048 rows of 4096 bfloat16: 9.4 us with two vectors, 9.9 with one; 256 rows of 2048: 3.8 and 3.6).  Backward: one vector a
+// thread wherever there is a shape for it, for the registers (16384 rows of 2048 bfloat16: 43.8 us with two, 41 with one).
+static int rows_choice(long long outer, int C, int vec, bool backward)
+{
+    for (int pass = backward || outer < 2048 ? 0 : 1; pass < 2; ++pass)
+        for (int i = 0; i < kNormRowsShapes; ++i)
+            if (rows_fit(i, C, vec, backward) && (pass == 1 || kNormRows[i].k == 1)) return i;
+    return -1;
+}
+
+// Maps: four channels a thread, so that a tile is small and many are under way (8 images of 96 channels, 55 x 55, binary32, backward: 11.5 us,
+// with eight 12.9), except 17 to 32 channels, where a wave then has the pixels of a line to itself (64 images of 32, 112 x 112, forward: 44 us against
+// 48 and backward 69 against 71), and the forward pass over 129 to 256 (64 images of 256, 14 x 14, bfloat16: 7.7 against 8.3).
+static int maps_choice(int C, bool one, bool backward)
+{
+    for (int i = 0; i < kNormMapsShapes; ++i) {
+        const bool eight = kNormMaps[i].k == 8 && kNormMaps[i].cg < 256;
+        const bool wanted = kNormMaps[i].cg == 4 ? C > 16 : !backward && C > 128;
+        if (maps_fit(i, C, one) && (!eight || wanted)) return i;
+    }
+    return -1;
+}
+
+// How many workgroups: forward, enough to fill the chip several times over; backward, two for each of the 256 CUs, since each writes its sums of the
+// parameters' gradients (16384 rows of 4096 bfloat16 in a join: 256 workgroups 149 us, 512 136, 1024 143).
+// The parameters' gradients are made aside up to 1024 rows or 4096 pixels and 8 MB (777 rows of 1021 binary32: 7.6 us against 10.3; 1024 rows of 4096
+// bfloat16 17.2 and 18.8; 2048 rows of 1021 14.9 and 13.9; 16 maps of 256 channels, 14 x 14: 7.8 and 10.7, 32 maps 11.4 and 11.9).
+constexpr int kForwardBlocks = 4096, kBackwardBlocks = 512;
 
 NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, bool backward, int variant)
 {
     const long long positions = outer * inner;
-    const int vec = type == DWM_F32 ? 4 : 8;
-    const NormShape any = any_shape(positions, C, inner == 1), none{-1, 0};
+    const NormShape any = any_shape(positions, C, inner == 1), none{-1, 0, false};
     if (variant == kNormAny || (variant < 0 && positions == 0)) return any;
+    const int size = type == DWM_F32 ? 4 : 2, most = backward ? kBackwardBlocks : kForwardBlocks;
+    const bool small = positions * C * size <= 8 << 20;
     if (inner == 1) {
-        int shape = variant - kNormRowsFirst;
-        if (variant < 0)
-            for (shape = 0; shape < kNormRowsShapes && kNormRows[shape].tpr * kNormRows[shape].k * vec < C;) ++shape;
-        const bool ok = shape >= 0 && shape < kNormRowsShapes && kNormRows[shape].tpr * kNormRows[shape].k * vec >= C && C >= vec;
-        if (!ok) return variant < 0 ? any : none;
+        const int vec = 16 / size, shape = variant < 0 ? rows_choice(outer, C, vec, backward) : variant - kNormRowsFirst;
+        if (!rows_fit(shape, C, vec, backward)) return variant < 0 ? any : none;
         const int tpr = kNormRows[shape].tpr, smallest = backward ? kNormRowsBackwardThreads : 256;
         const int rows = (tpr > smallest ? tpr : smallest) / tpr;
-        const long long blocks = (outer + rows - 1) / rows;
-        return {kNormRowsFirst + shape, (int)at_most(blocks, backward ? 512 : 2048)};
+        return {kNormRowsFirst + shape, (int)at_most((outer + rows - 1) / rows, most), small && outer <= 1024};
     }
-    bool one = variant < 0 ? inner < vec : variant >= kNormMapsOne;
-    int shape = variant - (one ? kNormMapsOne : kNormMapsVec);
-    if (variant < 0)
-        for (shape = 0; shape < kNormMapsShapes && kNormMaps[shape].cg * kNormMaps[shape].k < C;) ++shape;
-    const long long vectors = one ? positions : outer * ((inner + vec - 1) / vec), limit = (1LL << 31) - 1;
-    const bool ok = shape >= 0 && shape < kNormMapsShapes && kNormMaps[shape].cg * kNormMaps[shape].k >= C && (one || inner >= vec) &&
-                    vectors < limit && inner < limit;
-    if (!ok) return variant < 0 ? any : none;
+    // One pixel a lane where there are fewer than four, and up to 2^20 elements, where four leave CUs without work (one image of 256 channels, 28 x 28,
+    // bfloat16, forward: 4.2 us against 7.2; 8 images 5.5 both; 64 of 14 x 14 9.6 against 7.7).
+    const bool one = variant < 0 ? inner < kNormMapsPixels || positions * C <= 1 << 20 : variant >= kNormMapsOne;
+    const int shape = variant < 0 ? maps_choice(C, one, backward) : variant - (one ? kNormMapsOne : kNormMapsVec);
+    const long long vectors = one ? positions : outer * ((inner + kNormMapsPixels - 1) / kNormMapsPixels), limit = (1LL << 31) - 1;
+    if (!maps_fit(shape, C, one) || !(one || inner >= kNormMapsPixels) || vectors >= limit || inner >= limit) return variant < 0 ? any : none;
     const long long tiles = (vectors + kNormMaps[shape].pl - 1) / kNormMaps[shape].pl;
-    return {(one ? kNormMapsOne : kNormMapsVec) + shape, (int)at_most(tiles, backward ? 512 : 4096)};
+    return {(one ? kNormMapsOne : kNormMapsVec) + shape, (int)at_most(tiles, most), small && positions <= 4096};
 }
 
 static const char* const kTensorNames[kNormTensors] = {"x", "residual", "z", "y", "dy", "dz", "dx", "dresidual"};
@@ -126,13 +165,25 @@ static dwm_status_t run_forward(const dwm_norm_plan& p, const NormArgs& a, bool 
     return p.forward.kernel == kNormAny ? launch_norm_any_forward(a, p.type, join, stream) : run_kernel(p, a, p.forward, false, join, stream);
 }
 
-static dwm_status_t run_backward(const dwm_norm_plan& p, const NormArgs& a, void* stream)
+static dwm_status_t run_backward(const dwm_norm_plan& p, const NormArgs& a, bool join, void* stream)
 {
     const bool params = a.dgamma || a.dbeta;
     if (params && !p.ws) return DWM_ERR_WORKSPACE;
     if (p.backward.kernel == kNormAny) return launch_norm_any_backward(a, p.type, stream);
-    const dwm_status_t st = run_kernel(p, a, p.backward, true, false, stream);
-    return st != DWM_OK || !params ? st : launch_norm_params_final(a, p.type, stream);
+    NormArgs b = a;
+    if (!params || p.backward.aside) b.partial = nullptr;
+    if (params && p.backward.aside) {
+        b.aside = 1;
+        if (a.dy == a.dx || a.dy == a.dresidual) {  // dy would be overwritten while it is read: the parameters' gradients first
+            b.splits = 0;
+            const dwm_status_t st = run_kernel(p, b, p.backward, true, join, stream);
+            if (st != DWM_OK) return st;
+            b.splits = a.splits;
+            b.aside = 0;
+        }
+    }
+    const dwm_status_t st = run_kernel(p, b, p.backward, true, join, stream);
+    return st != DWM_OK || !b.partial ? st : launch_norm_params_final(a, p.type, stream);
 }
 
 }  // namespace dwm
@@ -258,7 +309,7 @@ dwm_status_t dwm_norm_backward(const dwm_norm_plan_t* plan, const void* dy_dev, 
     a.stride[kNormDresidual] = plan->stride[kNormDx];
     a.dgamma = dgamma_dev;
     a.dbeta = dbeta_dev;
-    return run_backward(*plan, a, stream);
+    return run_backward(*plan, a, false, stream);
 }
 
 dwm_status_t dwm_norm_join_forward(const dwm_norm_plan_t* plan, const dwm_dropout_t* drop, const void* x_dev,
@@ -307,7 +358,7 @@ dwm_status_t dwm_norm_join_backward(const dwm_norm_plan_t* plan, const dwm_dropo
     a.dresidual = dresidual_dev;
     a.dgamma = dgamma_dev;
     a.dbeta = dbeta_dev;
-    return run_backward(*plan, a, stream);
+    return run_backward(*plan, a, true, stream);
 }
 
 dwm_status_t dwm_dropout_forward(const dwm_dropout_t* drop, dwm_type_t type, long long n, const void* x_dev, void* y_dev,

@@ -31,33 +31,43 @@ struct NormArgs {
     long long outer, inner;
     int C;
     int param_typed;  // parameters have the tensors' type, otherwise binary32
-    int splits;
+    int splits;       // workgroups of a backward kernel for the gradient of z
+    int aside;        // behind them, others for the parameters' gradients; `partial` is null then
     float eps;
     DropArgs drop;
 };
 
-// The shapes that the register-resident kernels (norm_impl.inc) are built in.  Rows: threads of a row, vectors of sixteen bytes of a
-// thread.  Maps: lanes along the pixels, groups along the channels, channels of a thread.
+// The shapes that the register-resident kernels (norm_impl.inc) are built in, from the narrowest to the widest.  Rows: threads of a row, vectors of
+// sixteen bytes of a thread, and in which directions the shape is built.  Maps: lanes along the pixels, groups along the channels,
+// channels of a thread, and whether it is built with one pixel a lane too.
 struct NormRows {
     int tpr, k;
+    bool forward, backward;
 };
 struct NormMaps {
     int pl, cg, k;
+    bool one;
 };
-constexpr NormRows kNormRows[] = {{8, 1}, {16, 1}, {32, 1}, {64, 1}, {64, 2}, {64, 4}, {256, 1}, {256, 2}, {256, 4}, {1024, 1}, {1024, 2}, {1024, 4}};
-constexpr NormMaps kNormMaps[] = {{64, 4, 8}, {16, 16, 8}, {16, 32, 8}, {16, 64, 8}, {16, 64, 16}};
+constexpr NormRows kNormRows[] = {
+    {8, 1, true, true},    {16, 1, true, true},   {32, 1, true, true},   {64, 1, true, true},   {64, 2, true, false},  {128, 1, true, true},   {128, 2, true, false},
+    {256, 1, true, true},  {256, 2, true, false}, {512, 1, true, true},  {512, 2, true, true},  {1024, 2, true, true}, {1024, 4, true, true},
+};
+constexpr NormMaps kNormMaps[] = {
+    {64, 4, 4, true}, {64, 4, 8, false}, {16, 16, 4, true}, {8, 32, 4, true}, {8, 32, 8, false}, {8, 64, 4, true}, {4, 128, 4, true}, {4, 256, 4, true}, {4, 256, 8, true},
+};
 constexpr int kNormRowsShapes = sizeof(kNormRows) / sizeof(kNormRows[0]), kNormMapsShapes = sizeof(kNormMaps) / sizeof(kNormMaps[0]);
 constexpr int kNormRowsBackwardThreads = 512;
+constexpr int kNormRowsWidest = 16384;  // channels that a backward kernel holds: the sums of dgamma and dbeta fill 128 KB of LDS
+constexpr int kNormMapsPixels = 4;      // of a lane
 
-// A plan's kernel: 0 (norm_any.hip), or a shape from here on of rows, of maps with sixteen bytes of pixels a lane, with one pixel a lane.
+// A plan's kernel: 0 (norm_any.hip), or a shape from here on of rows, of maps with four pixels a lane, with one.
 constexpr int kNormAny = 0, kNormRowsFirst = 1, kNormMapsVec = 100, kNormMapsOne = 200;
 
 struct NormShape {
     int kernel;
     int blocks;  // workgroups; backward: splits of the parameters' gradients too
+    bool aside;  // backward: the parameters' gradients by workgroups of their own in the same launch
 };
-
-constexpr int kNormMaxSplits = 1024;
 
 // The planner's choice (variant < 0), or the kernel asked for; kernel = -1: it does not apply.
 NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, bool backward, int variant);

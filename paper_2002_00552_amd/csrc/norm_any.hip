@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void norm_any_forward_kernel(NormArgs a)
         }
         s1 = position_sum<L>(s1, lds) * inv_c;
         s2 = position_sum<L>(s2, lds) * inv_c;
-        const NormStats st = norm_stats(m0, s1, s2, a.eps);
+        const NormStats st = norm_stats(m0, s1, s2 - s1 * s1, a.eps);
         T* yp = y + o * a.stride[kNormY] + i;
         for (int c = g; c < n; c += G) {
             const float d = (float)vp[c * a.inner] - m0 - st.off;
@@ -156,6 +156,7 @@ __global__ __launch_bounds__(1024) void norm_params_final_kernel(NormArgs a)
     const int c = blockIdx.x * 32 + lane;
     float sum = 0.0f;
     if (c < a.C)
+#pragma unroll 8
         for (int s = group; s < a.splits; s += 32) sum += a.partial[((long long)s * 2 + which) * a.C + c];
     lds[group][lane] = sum;
     __syncthreads();

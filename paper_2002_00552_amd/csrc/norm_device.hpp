@@ -19,12 +19,12 @@ template <class T, int V> __device__ __forceinline__ void params(const void* p, 
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = none;
     } else if (typed) {
-        unpack<T>(load16((const T*)p + c), f);
+        unpack<T, V>(load_vector<T, V>((const T*)p + c), f);
     } else {
 #pragma unroll
         for (int j = 0; j < V; j += 4) {
             float q[4];
-            unpack<float>(load16((const float*)p + c + j), q);
+            unpack<float, 4>(load_vector<float, 4>((const float*)p + c + j), q);
 #pragma unroll
             for (int i = 0; i < 4; ++i) f[j + i] = q[i];
         }
@@ -49,11 +49,11 @@ template <int STEP> __device__ __forceinline__ float add_across(float v)
     }
 }
 
-// The sum over N consecutive lanes (4 to 64), for all of them.
+// The sum over N consecutive lanes (2 to 64), for all of them.
 template <int N> __device__ __forceinline__ float lanes_sum(float v)
 {
     v += dpp<0xB1>(v);               // the neighbour of a pair
-    v += dpp<0x4E>(v);               // the other pair of four
+    if (N >= 4) v += dpp<0x4E>(v);   // the other pair of four
     if (N >= 8) v += dpp<0x141>(v);  // the other four of eight, mirrored: all four have the same sum
     if (N >= 16) v += dpp<0x140>(v);
     if (N >= 32) v = add_across<16>(v);
@@ -61,21 +61,44 @@ template <int N> __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 
-// From the first mean m0 (a sum times 1 / C) and the means s1, s2 of d and d^2, d = z - m0: what is taken off d for y (`off`),
-// the mean and rstd.  s1 is the rounding of m0, which counts where the mean is larger than the deviations; where it is smaller,
-// m0 is good to a fraction of the deviations' roundoff, and s1 holds the roundings of z - m0 instead, which all have
-// one sign where z has few bits (rows of bfloat16 with means of a hundredth: a mean off by 1e-6 of itself).
+// Sums over the lanes of a wave that are N apart, 2 N apart, ...: for all of them.
+template <int N> __device__ __forceinline__ float strided_sum(float v)
+{
+    if (N <= 4) v += dpp<0x124>(v);  // four lanes on, round in sixteen
+    if (N <= 8) v += dpp<0x128>(v);  // eight
+    if (N <= 16) v = add_across<16>(v);
+    if (N <= 32) v = add_across<32>(v);
+    return v;
+}
+
+// The statistics of a norm from a first mean m0, the mean s1 of d = z - m0 and its variance: `off` is what is taken off d for y.
+// s1 is the rounding of m0, which counts where the mean is larger than the deviations; where it is smaller, m0 is good
+// to a fraction of the deviations' roundoff, and s1 holds the roundings of z - m0 instead, which all have one sign where z has few
+// bits (rows of bfloat16 with means of a hundredth: a mean off by 1e-6 of itself).
 struct NormStats {
     float off, mean, rstd;
 };
-__device__ __forceinline__ NormStats norm_stats(float m0, float s1, float s2, float eps)
+__device__ __forceinline__ NormStats norm_stats(float m0, float s1, float var, float eps)
 {
     NormStats r;
-    const float var = s2 - s1 * s1;
     r.rstd = 1.0f / sqrtf((var < 0.0f ? 0.0f : var) + eps);  // (NaN stays)
     r.off = fabsf(m0) * r.rstd > 1.0f ? s1 : 0.0f;
     r.mean = m0 + r.off;
     return r;
 }
+
+// A wave's share of a norm: how many elements it holds, their mean, and the sums of d and of d^2, d = z - mean (the first only by
+// the mean's rounding).  Shares are joined without a second reading of the elements: with m0 the mean of all, the sum of z - m0
+// over a share is n (mean - m0) + q1, which makes s1, and with u = mean - m0 - s1 the sum of (z - m0 - s1)^2 is q2 + 2 u q1 + n u^2: deviations
+// all of it, nothing cancels.
+struct NormShare {
+    float n, mean, q1, q2;
+    __device__ __forceinline__ float first(float m0) const { return n * (mean - m0) + q1; }
+    __device__ __forceinline__ float second(float m0, float s1) const
+    {
+        const float u = mean - m0 - s1;
+        return q2 + u * (2.0f * q1 + n * u);
+    }
+};
 
 }  // namespace dwm
