@@ -27,10 +27,13 @@ static bool rows_fit(int shape, int C, int vec, bool backward)
     const int holds = r.tpr * r.k * vec;
     return holds >= C && C >= vec && (backward ? r.backward && holds <= kNormRowsWidest : r.forward);
 }
-static bool maps_fit(int shape, int C, bool one)
+static bool maps_fit(int shape, int C, int size, bool one, bool backward)
 {
-    return shape >= 0 && shape < kNormMapsShapes && kNormMaps[shape].cg * kNormMaps[shape].k >= C && (!one || kNormMaps[shape].one);
+    if (shape < 0 || shape >= kNormMapsShapes) return false;
+    const NormMaps& m = kNormMaps[shape];
+    return m.cg * m.k >= C && (!one || m.one) && (!backward || size <= m.backward);
 }
+static long long maps_tiles(int shape, long long vectors) { return (vectors + kNormMaps[shape].pl - 1) / kNormMaps[shape].pl; }
 
 // Rows, forward: the narrowest shape; below 2048 rows those with one vector a thread, a shorter way from the first load to the last store
 // (2048 rows of 4096 bfloat16: 9.4 us with two vectors, 9.9 with one; 256 rows of 2048: 3.8 and 3.6).  Backward: one vector a
@@ -43,17 +46,23 @@ static int rows_choice(long long outer, int C, int vec, bool backward)
     return -1;
 }
 
-// Maps: four channels a thread, so that a tile is small and many are under way (8 images of 96 channels, 55 x 55, binary32, backward: 11.5 us,
-// with eight 12.9), except 17 to 32 channels, where a wave then has the pixels of a line to itself (64 images of 32, 112 x 112, forward: 44 us against
-// 48 and backward 69 against 71), and the forward pass over 129 to 256 (64 images of 256, 14 x 14, bfloat16: 7.7 against 8.3).
-static int maps_choice(int C, bool one, bool backward)
+// Maps: four channels a thread, so that a tile is small and many are under way, or, where tiles of eight channels a thread are still enough
+// for the chip, those, whose lanes lie along more pixels.  us, four and eight, forward: 64 images of 1024 channels, 14 x 14, binary32: 35.3,
+// 30.0; of 7 x 7: 12.3, 13.9; 64 of 512, 14 x 14, binary32: 18.0, 15.6; 8 images of 96, 55 x 55, bfloat16: 6.3, 6.8; 64 of them: 22.0, 20.7.
+// Backward in binary32 eight do not pay (64 images of 256, 28 x 28: 39.4, 45.9), with 16 bits from twice the size on (64 of 96, 55 x 55: 39.1, 33.8;
+// of 128, 28 x 28: 15.5, 16.4).  In the forward pass over 129 to 256 channels and in both over 17 to 32 eight always do (64 images of
+// 256, 14 x 14, bfloat16: 8.3, 7.7; of 32, 112 x 112, binary32: 48, 44 and 71, 69).
+static int maps_choice(int C, int size, long long vectors, bool one, bool backward)
 {
-    for (int i = 0; i < kNormMapsShapes; ++i) {
-        const bool eight = kNormMaps[i].k == 8 && kNormMaps[i].cg < 256;
-        const bool wanted = kNormMaps[i].cg == 4 ? C > 16 : !backward && C > 128;
-        if (maps_fit(i, C, one) && (!eight || wanted)) return i;
-    }
-    return -1;
+    int four = -1, eight = -1;
+    for (int i = kNormMapsShapes - 1; i >= 0; --i)
+        if (maps_fit(i, C, size, one, backward)) (kNormMaps[i].k == 4 ? four : eight) = i;
+    if (four < 0 || eight < 0) return four < 0 ? eight : four;
+    const NormMaps &m = kNormMaps[eight], &n = kNormMaps[four];
+    if (m.cg == 4) return C > 16 ? eight : four;
+    if (m.cg * m.k > n.cg * n.k) return four;  // (made for more channels)
+    const long long threads = maps_tiles(eight, vectors) * m.pl * m.cg, enough = 256 * 768;
+    return (m.cg == 32 && C > 128) || threads >= (backward ? 2 : 1) * enough ? eight : four;
 }
 
 // How many workgroups: forward, enough to fill the chip several times over; backward, two for each of the 256 CUs, since each writes its sums of the
@@ -69,7 +78,8 @@ NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, 
     if (variant == kNormAny || (variant < 0 && positions == 0)) return any;
     const int size = type == DWM_F32 ? 4 : 2, most = backward ? kBackwardBlocks : kForwardBlocks;
     const bool small = positions * C * size <= 8 << 20;
-    if (inner == 1) {
+    // (rows shorter than a vector are taken as maps of one pixel)
+    if (inner == 1 && (variant < 0 ? C >= 16 / size : variant < kNormMapsVec)) {
         const int vec = 16 / size, shape = variant < 0 ? rows_choice(outer, C, vec, backward) : variant - kNormRowsFirst;
         if (!rows_fit(shape, C, vec, backward)) return variant < 0 ? any : none;
         const int tpr = kNormRows[shape].tpr, smallest = backward ? kNormRowsBackwardThreads : 256;
@@ -79,11 +89,11 @@ NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, 
     // One pixel a lane where there are fewer than four, and up to 2^20 elements, where four leave CUs without work (one image of 256 channels, 28 x 28,
     // bfloat16, forward: 4.2 us against 7.2; 8 images 5.5 both; 64 of 14 x 14 9.6 against 7.7).
     const bool one = variant < 0 ? inner < kNormMapsPixels || positions * C <= 1 << 20 : variant >= kNormMapsOne;
-    const int shape = variant < 0 ? maps_choice(C, one, backward) : variant - (one ? kNormMapsOne : kNormMapsVec);
     const long long vectors = one ? positions : outer * ((inner + kNormMapsPixels - 1) / kNormMapsPixels), limit = (1LL << 31) - 1;
-    if (!maps_fit(shape, C, one) || !(one || inner >= kNormMapsPixels) || vectors >= limit || inner >= limit) return variant < 0 ? any : none;
-    const long long tiles = (vectors + kNormMaps[shape].pl - 1) / kNormMaps[shape].pl;
-    return {(one ? kNormMapsOne : kNormMapsVec) + shape, (int)at_most(tiles, most), small && positions <= 4096};
+    const int shape = variant < 0 ? maps_choice(C, size, vectors, one, backward) : variant - (one ? kNormMapsOne : kNormMapsVec);
+    if (!maps_fit(shape, C, size, one, backward) || !(one || inner >= kNormMapsPixels) || vectors >= limit || inner >= limit)
+        return variant < 0 ? any : none;
+    return {(one ? kNormMapsOne : kNormMapsVec) + shape, (int)at_most(maps_tiles(shape, vectors), most), small && positions <= 4096};
 }
 
 static const char* const kTensorNames[kNormTensors] = {"x", "residual", "z", "y", "dy", "dz", "dx", "dresidual"};

@@ -32,28 +32,30 @@ struct NormArgs {
     int C;
     int param_typed;  // parameters have the tensors' type, otherwise binary32
     int splits;       // workgroups of a backward kernel for the gradient of z
-    int aside;        // behind them, others for the parameters' gradients; `partial` is null then
+    int aside;        // in front of them, others for the parameters' gradients (their number, set at the launch); `partial` is null then
     float eps;
     DropArgs drop;
 };
 
 // The shapes that the register-resident kernels (norm_impl.inc) are built in, from the narrowest to the widest.  Rows: threads of a row, vectors of
 // sixteen bytes of a thread, and in which directions the shape is built.  Maps: lanes along the pixels, groups along the channels,
-// channels of a thread, and whether it is built with one pixel a lane too.
+// channels of a thread.
 struct NormRows {
     int tpr, k;
     bool forward, backward;
 };
 struct NormMaps {
     int pl, cg, k;
-    bool one;
+    bool one;       // with one pixel a lane too
+    int backward;   // the largest element size of a backward kernel
 };
 constexpr NormRows kNormRows[] = {
     {8, 1, true, true},    {16, 1, true, true},   {32, 1, true, true},   {64, 1, true, true},   {64, 2, true, false},  {128, 1, true, true},   {128, 2, true, false},
     {256, 1, true, true},  {256, 2, true, false}, {512, 1, true, true},  {512, 2, true, true},  {1024, 2, true, true}, {1024, 4, true, true},
 };
 constexpr NormMaps kNormMaps[] = {
-    {64, 4, 4, true}, {64, 4, 8, false}, {16, 16, 4, true}, {8, 32, 4, true}, {8, 32, 8, false}, {8, 64, 4, true}, {4, 128, 4, true}, {4, 256, 4, true}, {4, 256, 8, true},
+    {64, 4, 4, true, 4}, {64, 4, 8, false, 4}, {16, 16, 4, true, 4},  {8, 32, 4, true, 4},  {16, 16, 8, false, 2}, {8, 32, 8, false, 0},
+    {8, 64, 4, true, 4}, {4, 128, 4, true, 4}, {8, 64, 8, false, 2}, {4, 256, 4, true, 4}, {8, 128, 8, false, 2}, {4, 256, 8, true, 4},
 };
 constexpr int kNormRowsShapes = sizeof(kNormRows) / sizeof(kNormRows[0]), kNormMapsShapes = sizeof(kNormMaps) / sizeof(kNormMaps[0]);
 constexpr int kNormRowsBackwardThreads = 512;

@@ -8,7 +8,7 @@
 // that keep a norm in registers (norm_impl.inc) take every size that they can.  Sums are in binary32.  The second pass takes the
 // sums of d and of d^2, d = z - m; the first of them tells how far m was off (norm_device.hpp).
 // A workgroup owns L positions next to each other, 256 / L threads each: lanes lie along what is contiguous, the channels of a
-// row (L = 1) or the pixels of a map (L = 64).  A thread meets the same elements in every pass, so z may be the residual's own
+// row (L = 1) or the pixels of a map (L = 64 or 8).  A thread meets the same elements in every pass, so z may be the residual's own
 // memory, and what a pass wrote is there for the next.
 #include "norm_device.hpp"
 
@@ -176,14 +176,24 @@ static dwm_status_t params_final(const NormArgs& a, hipStream_t stream)
     return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
 }
 
+// Pixels of a workgroup: a wave's 64, or eight where those would be few workgroups.
+static int lanes(const NormArgs& a) { return a.inner == 1 ? 1 : a.outer * a.inner >= 64 * 2048 ? 64 : 8; }
+
 template <class T, int L>
-static dwm_status_t forward(const NormArgs& a, bool join, hipStream_t stream)
+static dwm_status_t forward_lanes(const NormArgs& a, bool join, hipStream_t stream)
 {
     const long long tiles = (a.outer * a.inner + L - 1) / L;
     const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20));
     if (join) hipLaunchKernelGGL((norm_any_forward_kernel<T, L, true>), grid, dim3(256), 0, stream, a);
     else hipLaunchKernelGGL((norm_any_forward_kernel<T, L, false>), grid, dim3(256), 0, stream, a);
     return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
+}
+
+template <class T>
+static dwm_status_t forward(const NormArgs& a, bool join, hipStream_t stream)
+{
+    const int L = lanes(a);
+    return L == 1 ? forward_lanes<T, 1>(a, join, stream) : L == 8 ? forward_lanes<T, 8>(a, join, stream) : forward_lanes<T, 64>(a, join, stream);
 }
 
 template <class T>
@@ -200,10 +210,11 @@ static dwm_status_t backward(const NormArgs& a, hipStream_t stream)
         if (st != DWM_OK) return st;
     }
     if ((a.dx || a.dresidual) && positions > 0) {
-        const int L = a.inner == 1 ? 1 : 64;
+        const int L = lanes(a);
         const long long tiles = (positions + L - 1) / L;
         const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20));
         if (L == 1) hipLaunchKernelGGL((norm_any_backward_kernel<T, 1>), grid, dim3(256), 0, stream, a);
+        else if (L == 8) hipLaunchKernelGGL((norm_any_backward_kernel<T, 8>), grid, dim3(256), 0, stream, a);
         else hipLaunchKernelGGL((norm_any_backward_kernel<T, 64>), grid, dim3(256), 0, stream, a);
         if (hipGetLastError() != hipSuccess) return DWM_ERR_HIP;
     }
@@ -215,9 +226,9 @@ dwm_status_t launch_norm_any_forward(const NormArgs& a, dwm_type_t type, bool jo
     const hipStream_t s = (hipStream_t)stream;
     if (a.outer == 0) return DWM_OK;
     switch (type) {
-        case DWM_F32: return a.inner == 1 ? forward<float, 1>(a, join, s) : forward<float, 64>(a, join, s);
-        case DWM_F16: return a.inner == 1 ? forward<_Float16, 1>(a, join, s) : forward<_Float16, 64>(a, join, s);
-        case DWM_BF16: return a.inner == 1 ? forward<__bf16, 1>(a, join, s) : forward<__bf16, 64>(a, join, s);
+        case DWM_F32: return forward<float>(a, join, s);
+        case DWM_F16: return forward<_Float16>(a, join, s);
+        case DWM_BF16: return forward<__bf16>(a, join, s);
     }
     return DWM_ERR_INVALID_ARG;
 }

@@ -458,12 +458,12 @@ def test_offsets_beyond_32_bits(shape):
         dwm.dwm_norm_plan_destroy(plan)
 
 
-KERNELS = [*range(0, 14), *range(100, 109), *range(200, 209)]  # dwm_norm_set_variant's numbers
+KERNELS = [*range(0, 14), *range(100, 112), *range(200, 212)]  # dwm_norm_set_variant's numbers
 
 
 @pytest.mark.parametrize("stage", ["forward", "backward"])
-@pytest.mark.parametrize("shape, some", [((70, 40, 1), 4), ((9, 61, 1), 4), ((1500, 1000, 1), 4), ((3, 8190, 1), 2), ((3, 16381, 1), 1), ((6, 32, 49), 14),
-                                         ((300, 100, 18), 9), ((2, 700, 270), 4), ((7, 90, 6), 9), ((2, 1999, 5), 2)],
+@pytest.mark.parametrize("shape, some", [((70, 40, 1), 4), ((9, 61, 1), 4), ((1500, 1000, 1), 4), ((3, 8190, 1), 2), ((3, 16381, 1), 1), ((6, 32, 49), 12),
+                                         ((300, 100, 18), 6), ((2, 700, 270), 3), ((7, 90, 6), 6), ((2, 1999, 5), 2), ((2500, 3, 1), 3)],
                          ids=lambda s: "x".join(map(str, s)) if isinstance(s, tuple) else str(s))
 def test_every_kernel(shape, some, stage, monkeypatch):
     """Each kernel that can hold the channels, asked for by number, in training and in a join: at least `some` of them."""
@@ -492,4 +492,4 @@ def test_every_kernel(shape, some, stage, monkeypatch):
             check(shape, dtype, "f32", kind="offset")
             check(shape, dtype, dtype, join=True, p=0.2, wide=5)
             monkeypatch.undo()
-        assert taken > some - (dtype != "f32" and stage == "backward" and shape[1] > 8192), taken
+        assert taken > some, taken
