@@ -65,26 +65,26 @@ static int maps_choice(int C, int size, long long vectors, bool one, bool backwa
     return (m.cg == 32 && C > 128) || threads >= (backward ? 2 : 1) * enough ? eight : four;
 }
 
-// How many workgroups: forward, enough to fill the chip several times over; backward, two for each of the 256 CUs, since each writes its sums of the
-// parameters' gradients (16384 rows of 4096 bfloat16 in a join: 256 workgroups 149 us, 512 136, 1024 143).
+// How many workgroups: forward, enough to fill the chip several times over; backward over maps, two for each of the 256 CUs, since each writes its
+// sums of the parameters' gradients (32 images of 256 channels, 28 x 28, binary32: 256 workgroups 29.9 us, 512 24.4, 1024 25.2).
 // The parameters' gradients are made aside up to 1024 rows or 4096 pixels and 8 MB (777 rows of 1021 binary32: 7.6 us against 10.3; 1024 rows of 4096
 // bfloat16 17.2 and 18.8; 2048 rows of 1021 14.9 and 13.9; 16 maps of 256 channels, 14 x 14: 7.8 and 10.7, 32 maps 11.4 and 11.9).
-constexpr int kForwardBlocks = 4096, kBackwardBlocks = 512;
+constexpr int kForwardBlocks = 4096, kMapsBackwardBlocks = 512;
 
 NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, bool backward, int variant)
 {
     const long long positions = outer * inner;
     const NormShape any = any_shape(positions, C, inner == 1), none{-1, 0, false};
     if (variant == kNormAny || (variant < 0 && positions == 0)) return any;
-    const int size = type == DWM_F32 ? 4 : 2, most = backward ? kBackwardBlocks : kForwardBlocks;
+    const int size = type == DWM_F32 ? 4 : 2;
     const bool small = positions * C * size <= 8 << 20;
     // (rows shorter than a vector are taken as maps of one pixel)
     if (inner == 1 && (variant < 0 ? C >= 16 / size : variant < kNormMapsVec)) {
         const int vec = 16 / size, shape = variant < 0 ? rows_choice(outer, C, vec, backward) : variant - kNormRowsFirst;
         if (!rows_fit(shape, C, vec, backward)) return variant < 0 ? any : none;
-        const int tpr = kNormRows[shape].tpr, smallest = backward ? kNormRowsBackwardThreads : 256;
-        const int rows = (tpr > smallest ? tpr : smallest) / tpr;
-        return {kNormRowsFirst + shape, (int)at_most((outer + rows - 1) / rows, most), small && outer <= 1024};
+        const int tpr = kNormRows[shape].tpr, threads = backward ? norm_rows_threads(kNormRows[shape], C % vec != 0) : tpr > 256 ? tpr : 256;
+        const long long blocks = (outer + threads / tpr - 1) / (threads / tpr);
+        return {kNormRowsFirst + shape, (int)at_most(blocks, backward ? norm_rows_blocks(threads) : kForwardBlocks), small && outer <= 1024};
     }
     // One pixel a lane where there are fewer than four, and up to 2^20 elements, where four leave CUs without work (one image of 256 channels, 28 x 28,
     // bfloat16, forward: 4.2 us against 7.2; 8 images 5.5 both; 64 of 14 x 14 9.6 against 7.7).
@@ -93,7 +93,7 @@ NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, 
     const int shape = variant < 0 ? maps_choice(C, size, vectors, one, backward) : variant - (one ? kNormMapsOne : kNormMapsVec);
     if (!maps_fit(shape, C, size, one, backward) || !(one || inner >= kNormMapsPixels) || vectors >= limit || inner >= limit)
         return variant < 0 ? any : none;
-    return {(one ? kNormMapsOne : kNormMapsVec) + shape, (int)at_most(maps_tiles(shape, vectors), most), small && positions <= 4096};
+    return {(one ? kNormMapsOne : kNormMapsVec) + shape, (int)at_most(maps_tiles(shape, vectors), backward ? kMapsBackwardBlocks : kForwardBlocks), small && positions <= 4096};
 }
 
 static const char* const kTensorNames[kNormTensors] = {"x", "residual", "z", "y", "dy", "dz", "dx", "dresidual"};

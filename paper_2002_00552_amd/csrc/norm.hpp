@@ -58,7 +58,13 @@ constexpr NormMaps kNormMaps[] = {
     {8, 64, 4, true, 4}, {4, 128, 4, true, 4}, {8, 64, 8, false, 2}, {4, 256, 4, true, 4}, {8, 128, 8, false, 2}, {4, 256, 8, true, 4},
 };
 constexpr int kNormRowsShapes = sizeof(kNormRows) / sizeof(kNormRows[0]), kNormMapsShapes = sizeof(kNormMaps) / sizeof(kNormMaps[0]);
-constexpr int kNormRowsBackwardThreads = 512;
+
+// Threads of a backward workgroup over rows, and how many workgroups at most: each writes its sums of the parameters' gradients.  One of 1024 on
+// each CU where a wave or more hold a row in one vector a thread, without an odd end; two of 512 elsewhere, for the registers and the
+// sums over many short rows (a join in bfloat16, us, 512 and 1024 threads: 16384 rows of 4096 144, 129; 65536 of 2048 277, 248; of 1500
+// 257, 292; 2048 of 64 8.2, 10.2; 16384 of 8192, two vectors a thread, 252, 439).
+constexpr int norm_rows_threads(NormRows r, bool tail) { return r.tpr > 512 || (r.tpr >= 128 && r.k == 1 && !tail) ? 1024 : 512; }
+constexpr int norm_rows_blocks(int threads) { return 256 * 1024 / threads; }
 constexpr int kNormRowsWidest = 16384;  // channels that a backward kernel holds: the sums of dgamma and dbeta fill 128 KB of LDS
 constexpr int kNormMapsPixels = 4;      // of a lane
 
