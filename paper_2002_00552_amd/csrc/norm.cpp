@@ -8,7 +8,7 @@
 
 namespace dwm {
 
-static long long at_most(long long v, long long most) { return v < most ? v : most; }
+static int workgroups(long long v, int most) { return v < 1 ? 1 : v < most ? (int)v : most; }
 
 // norm_any.hip: splits of the positions for the parameters' gradients, enough for the chip, none without some work.
 static NormShape any_shape(long long positions, int C, bool rows)
@@ -16,7 +16,7 @@ static NormShape any_shape(long long positions, int C, bool rows)
     const long long groups = rows ? (C + 63) / 64 : C, threads = rows ? 4 : 256;
     long long splits = (positions + 16 * threads - 1) / (16 * threads);
     if (splits * groups > 4096) splits = 4096 / groups;
-    return {kNormAny, (int)(splits < 1 ? 1 : at_most(splits, 256)), false};
+    return {kNormAny, workgroups(splits, 256), false};
 }
 
 // Whether a shape can hold the norms of a plan.
@@ -84,16 +84,16 @@ NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, 
         if (!rows_fit(shape, C, vec, backward)) return variant < 0 ? any : none;
         const int tpr = kNormRows[shape].tpr, threads = backward ? norm_rows_threads(kNormRows[shape], C % vec != 0) : tpr > 256 ? tpr : 256;
         const long long blocks = (outer + threads / tpr - 1) / (threads / tpr);
-        return {kNormRowsFirst + shape, (int)at_most(blocks, backward ? norm_rows_blocks(threads) : kForwardBlocks), small && outer <= 1024};
+        return {kNormRowsFirst + shape, workgroups(blocks, backward ? norm_rows_blocks(threads) : kForwardBlocks), small && outer <= 1024};
     }
     // One pixel a lane where there are fewer than four, and up to 2^20 elements, where four leave CUs without work (one image of 256 channels, 28 x 28,
     // bfloat16, forward: 4.2 us against 7.2; 8 images 5.5 both; 64 of 14 x 14 9.6 against 7.7).
     const bool one = variant < 0 ? inner < kNormMapsPixels || positions * C <= 1 << 20 : variant >= kNormMapsOne;
-    const long long vectors = one ? positions : outer * ((inner + kNormMapsPixels - 1) / kNormMapsPixels), limit = (1LL << 31) - 1;
+    const long long vectors = one ? positions : outer * ((inner + kNormMapsPixels - 1) / kNormMapsPixels), limit = (1LL << 31) - 64;  // (indexes in 32 bits)
     const int shape = variant < 0 ? maps_choice(C, size, vectors, one, backward) : variant - (one ? kNormMapsOne : kNormMapsVec);
     if (!maps_fit(shape, C, size, one, backward) || !(one || inner >= kNormMapsPixels) || vectors >= limit || inner >= limit)
         return variant < 0 ? any : none;
-    return {(one ? kNormMapsOne : kNormMapsVec) + shape, (int)at_most(maps_tiles(shape, vectors), backward ? kMapsBackwardBlocks : kForwardBlocks), small && positions <= 4096};
+    return {(one ? kNormMapsOne : kNormMapsVec) + shape, workgroups(maps_tiles(shape, vectors), backward ? kMapsBackwardBlocks : kForwardBlocks), small && positions <= 4096};
 }
 
 static const char* const kTensorNames[kNormTensors] = {"x", "residual", "z", "y", "dy", "dz", "dx", "dresidual"};

@@ -315,6 +315,24 @@ def test_no_rows():
         norm.close()
 
 
+@pytest.mark.parametrize("shape, variant", [((0, 300, 1), v) for v in (0, 5, 8, 10, 12)] + [((0, 40, 30), v) for v in (0, 103, 111, 203)])
+def test_no_rows_in_every_kind_of_kernel(shape, variant):
+    plan = dwm.dwm_norm_plan_create(*shape, dwm.DWM_F32, dwm.DWM_F32, 1e-5)
+    try:
+        for stage in ("forward", "backward"):
+            if not (variant == 5 and stage == "backward"):  # (a shape of the forward pass alone)
+                dwm.dwm_norm_set_variant(plan, stage, variant)
+        ws = torch.full((dwm.dwm_norm_workspace_bytes(plan) // 4 + 64,), float("nan"), device="cuda")
+        dwm.dwm_norm_set_workspace(plan, ws.data_ptr(), ws.numel() * 4)
+        dgamma, dbeta = (torch.full((shape[1],), float("nan"), device="cuda") for _ in range(2))
+        dwm.dwm_norm_forward(plan, None, None, None, None, None, None, _stream())
+        dwm.dwm_norm_backward(plan, None, None, None, None, None, None, _ptr(dgamma), _ptr(dbeta), _stream())
+        assert bool((dgamma == 0).all()) and bool((dbeta == 0).all())
+    finally:
+        torch.cuda.synchronize()
+        dwm.dwm_norm_plan_destroy(plan)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 7, 8, 9, 63, 255, 1023, 1024, 1025, 2047, 2049, 100003])
 def test_dropout(n, dtype):
