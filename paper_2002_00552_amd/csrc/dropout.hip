@@ -14,25 +14,19 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropArgs d, long long firs
     const long long e0 = first + ((long long)blockIdx.x * 256 + threadIdx.x) * V;
     if (e0 >= n) return;
     const uint64_t sequence = drop_sequence(d);
-    bool keep[V];
     if (e0 + V <= n) {
         const uint4v r = load_vector<T, V>(x + e0);
-        if (d.mode == kDropDraw) {
-            drop_draw<V, true>(d, sequence, (uint64_t)e0, keep);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) keep[j] = d.mode == kDropNone;
-        }
+        bool keep[V];
+        drop_keep<V>(d, sequence, (uint64_t)e0, true, keep);  // while the load is on its way
         float f[V];
         unpack<T, V>(r, f);
 #pragma unroll
         for (int j = 0; j < V; ++j) f[j] = drop_scaled(f[j], keep[j], d.scale);
         store_vector<T, V>(y + e0, pack<T, V>(f));
     } else {
-        drop_draw<V, true>(d, sequence, (uint64_t)e0, keep);
+        const uint32_t bits = drop_bits<V>(d, sequence, (uint64_t)e0, true);
         for (int j = 0; j < V; ++j)
-            if (e0 + j < n)
-                y[e0 + j] = (T)drop_scaled((float)x[e0 + j], d.mode == kDropNone || (d.mode == kDropDraw && keep[j]), d.scale);
+            if (e0 + j < n) y[e0 + j] = (T)drop_scaled((float)x[e0 + j], bits, j, d.scale);
     }
 }
 

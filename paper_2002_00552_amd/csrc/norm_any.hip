@@ -52,9 +52,8 @@ __global__ __launch_bounds__(256) void norm_any_forward_kernel(NormArgs a)
         for (int c = g; c < n; c += G) {
             float v = (float)xp[c * a.inner];
             if (JOIN) {
-                bool keep[1] = {a.drop.mode == kDropNone};
-                if (a.drop.mode == kDropDraw) drop_draw<1, false>(a.drop, sequence, (uint64_t)((o * a.C + c) * a.inner + i), keep);
-                const T r = (T)join_sum((float)rp[c * a.inner], drop_scaled(v, keep[0], a.drop.scale));
+                const uint32_t bits = drop_bits<1>(a.drop, sequence, (uint64_t)((o * a.C + c) * a.inner + i), false);
+                const T r = (T)join_sum((float)rp[c * a.inner], drop_scaled(v, bits, 0, a.drop.scale));
                 zp[c * a.inner] = r;
                 v = (float)r;
             }
@@ -115,9 +114,8 @@ __global__ __launch_bounds__(256) void norm_any_backward_kernel(NormArgs a)
             if (a.dz) d += (float)((const T*)a.dz)[o * a.stride[kNormDz] + i + at];
             if (a.dresidual) ((T*)a.dresidual)[o * a.stride[kNormDresidual] + i + at] = (T)d;
             if (a.dx) {
-                bool keep[1] = {a.drop.mode == kDropNone};
-                if (a.drop.mode == kDropDraw) drop_draw<1, false>(a.drop, sequence, (uint64_t)((o * a.C + c) * a.inner + i), keep);
-                ((T*)a.dx)[o * a.stride[kNormDx] + i + at] = (T)drop_scaled(d, keep[0], a.drop.scale);
+                const uint32_t bits = drop_bits<1>(a.drop, sequence, (uint64_t)((o * a.C + c) * a.inner + i), false);
+                ((T*)a.dx)[o * a.stride[kNormDx] + i + at] = (T)drop_scaled(d, bits, 0, a.drop.scale);
             }
         }
     }
