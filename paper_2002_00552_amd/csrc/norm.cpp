@@ -37,7 +37,8 @@ static long long maps_tiles(int shape, long long vectors) { return (vectors + kN
 
 // Rows, forward: the narrowest shape; below 2048 rows those with one vector a thread, a shorter way from the first load to the last store
 // (2048 rows of 4096 bfloat16: 9.4 us with two vectors, 9.9 with one; 256 rows of 2048: 3.8 and 3.6).  Backward: one vector a
-// thread wherever there is a shape for it, for the registers (16384 rows of 2048 bfloat16: 43.8 us with two, 41 with one).
+// thread wherever there is a shape for it (4096 rows of 1500 bfloat16: 21.7 us with two, 17.5 with one; 65536 of 1024: 83 and 81; 16384 of 2048: 44
+// both).
 static int rows_choice(long long outer, int C, int vec, bool backward)
 {
     for (int pass = backward || outer < 2048 ? 0 : 1; pass < 2; ++pass)
