@@ -491,7 +491,7 @@ typedef struct {
     long long outer;
     int C;
     long long inner;
-    int forward_kernel, backward_kernel; /* dwm_norm_set_variant's numbers */
+    int forward_kernel, join_forward_kernel, backward_kernel; /* dwm_norm_set_variant's numbers */
     int splits;                          /* parts of the positions whose sums of the parameters' gradients are added up last */
 } dwm_norm_info_t;
 

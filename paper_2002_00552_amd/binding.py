@@ -74,7 +74,8 @@ class dwm_dropout_t(ctypes.Structure):
 
 class dwm_norm_info_t(ctypes.Structure):
     _fields_ = [("outer", ctypes.c_longlong), ("C", ctypes.c_int), ("inner", ctypes.c_longlong),
-                ("forward_kernel", ctypes.c_int), ("backward_kernel", ctypes.c_int), ("splits", ctypes.c_int)]
+                ("forward_kernel", ctypes.c_int), ("join_forward_kernel", ctypes.c_int), ("backward_kernel", ctypes.c_int),
+                ("splits", ctypes.c_int)]
 
 
 _P = ctypes.c_void_p

@@ -52,9 +52,11 @@ static int rows_choice(long long outer, int C, int vec, bool backward)
 // 30.0; of 7 x 7: 12.3, 13.9; 64 of 512, 14 x 14, binary32: 18.0, 15.6; 8 images of 96, 55 x 55, bfloat16: 6.3, 6.8; 64 of them: 22.0, 20.7.
 // Backward in binary32 eight do not pay (64 images of 256, 28 x 28: 39.4, 45.9), with 16 bits from twice the size on (64 of 96, 55 x 55: 39.1, 33.8;
 // of 128, 28 x 28: 15.5, 16.4).  In the forward pass over 129 to 256 channels and in both over 17 to 32 eight always do (64 images of
-// 256, 14 x 14, bfloat16: 8.3, 7.7; of 32, 112 x 112, binary32: 48, 44 and 71, 69).
-static int maps_choice(int C, int size, long long vectors, bool one, bool backward)
+// 256, 14 x 14, bfloat16: 8.3, 7.7; of 32, 112 x 112, binary32: 48, 44 and 71, 69).  A join, which holds the residual and the draws too, does not over
+// more than 256 (64 images of 512, 14 x 14, binary32: 30.4, 40.5; of 1024: 67, 75), except with 16 bits over more than 512 (48.4, 41.7).
+static int maps_choice(int C, int size, long long vectors, bool one, NormStage stage)
 {
+    const bool backward = stage == kNormBackward;
     int four = -1, eight = -1;
     for (int i = kNormMapsShapes - 1; i >= 0; --i)
         if (maps_fit(i, C, size, one, backward)) (kNormMaps[i].k == 4 ? four : eight) = i;
@@ -62,6 +64,7 @@ static int maps_choice(int C, int size, long long vectors, bool one, bool backwa
     const NormMaps &m = kNormMaps[eight], &n = kNormMaps[four];
     if (m.cg == 4) return C > 16 ? eight : four;
     if (m.cg * m.k > n.cg * n.k) return four;  // (made for more channels)
+    if (stage == kNormJoinForward && C > 256 && (size == 4 || C <= 512)) return four;
     const long long threads = maps_tiles(eight, vectors) * m.pl * m.cg, enough = 256 * 768;
     return (m.cg == 32 && C > 128) || threads >= (backward ? 2 : 1) * enough ? eight : four;
 }
@@ -72,8 +75,9 @@ static int maps_choice(int C, int size, long long vectors, bool one, bool backwa
 // bfloat16 17.2 and 18.8; 2048 rows of 1021 14.9 and 13.9; 16 maps of 256 channels, 14 x 14: 7.8 and 10.7, 32 maps 11.4 and 11.9).
 constexpr int kForwardBlocks = 4096, kMapsBackwardBlocks = 512;
 
-NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, bool backward, int variant)
+NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, NormStage stage, int variant)
 {
+    const bool backward = stage == kNormBackward;
     const long long positions = outer * inner;
     const NormShape any = any_shape(positions, C, inner == 1), none{-1, 0, false};
     if (variant == kNormAny || (variant < 0 && positions == 0)) return any;
@@ -91,7 +95,7 @@ NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, 
     // bfloat16, forward: 4.2 us against 7.2; 8 images 5.5 both; 64 of 14 x 14 9.6 against 7.7).
     const bool one = variant < 0 ? inner < kNormMapsPixels || positions * C <= 1 << 20 : variant >= kNormMapsOne;
     const long long vectors = one ? positions : outer * ((inner + kNormMapsPixels - 1) / kNormMapsPixels), limit = (1LL << 31) - 64;  // (indexes in 32 bits)
-    const int shape = variant < 0 ? maps_choice(C, size, vectors, one, backward) : variant - (one ? kNormMapsOne : kNormMapsVec);
+    const int shape = variant < 0 ? maps_choice(C, size, vectors, one, stage) : variant - (one ? kNormMapsOne : kNormMapsVec);
     if (!maps_fit(shape, C, size, one, backward) || !(one || inner >= kNormMapsPixels) || vectors >= limit || inner >= limit)
         return variant < 0 ? any : none;
     return {(one ? kNormMapsOne : kNormMapsVec) + shape, workgroups(maps_tiles(shape, vectors), backward ? kMapsBackwardBlocks : kForwardBlocks), small && positions <= 4096};
@@ -123,7 +127,7 @@ static bool drop_args(const dwm_dropout_t* drop, DropArgs* out)
     return true;
 }
 
-static NormArgs args_of(const dwm_norm_plan& p, const NormShape& shape)
+static NormArgs args_of(const dwm_norm_plan& p)
 {
     NormArgs a{};
     std::memcpy(a.stride, p.stride, sizeof(a.stride));
@@ -131,7 +135,7 @@ static NormArgs args_of(const dwm_norm_plan& p, const NormShape& shape)
     a.inner = p.inner;
     a.C = p.C;
     a.param_typed = p.param_type == p.type && p.type != DWM_F32;
-    a.splits = shape.blocks;
+    a.splits = p.shape[kNormBackward].blocks;
     a.eps = p.eps;
     a.partial = (float*)p.ws;
     a.drop.scale = 1.0f;
@@ -173,27 +177,28 @@ static dwm_status_t run_kernel(const dwm_norm_plan& p, const NormArgs& a, const 
 static dwm_status_t run_forward(const dwm_norm_plan& p, const NormArgs& a, bool join, void* stream)
 {
     if (p.outer == 0) return DWM_OK;
-    return p.forward.kernel == kNormAny ? launch_norm_any_forward(a, p.type, join, stream) : run_kernel(p, a, p.forward, false, join, stream);
+    const NormShape& shape = p.shape[join ? kNormJoinForward : kNormForward];
+    return shape.kernel == kNormAny ? launch_norm_any_forward(a, p.type, join, stream) : run_kernel(p, a, shape, false, join, stream);
 }
 
 static dwm_status_t run_backward(const dwm_norm_plan& p, const NormArgs& a, bool join, void* stream)
 {
     const bool params = a.dgamma || a.dbeta;
     if (params && !p.ws) return DWM_ERR_WORKSPACE;
-    if (p.backward.kernel == kNormAny) return launch_norm_any_backward(a, p.type, stream);
+    if (p.shape[kNormBackward].kernel == kNormAny) return launch_norm_any_backward(a, p.type, stream);
     NormArgs b = a;
-    if (!params || p.backward.aside) b.partial = nullptr;
-    if (params && p.backward.aside) {
+    if (!params || p.shape[kNormBackward].aside) b.partial = nullptr;
+    if (params && p.shape[kNormBackward].aside) {
         b.aside = 1;
         if (a.dy == a.dx || a.dy == a.dresidual) {  // dy would be overwritten while it is read: the parameters' gradients first
             b.splits = 0;
-            const dwm_status_t st = run_kernel(p, b, p.backward, true, join, stream);
+            const dwm_status_t st = run_kernel(p, b, p.shape[kNormBackward], true, join, stream);
             if (st != DWM_OK) return st;
             b.splits = a.splits;
             b.aside = 0;
         }
     }
-    const dwm_status_t st = run_kernel(p, b, p.backward, true, join, stream);
+    const dwm_status_t st = run_kernel(p, b, p.shape[kNormBackward], true, join, stream);
     return st != DWM_OK || !b.partial ? st : launch_norm_params_final(a, p.type, stream);
 }
 
@@ -219,8 +224,7 @@ dwm_status_t dwm_norm_plan_create(dwm_norm_plan_t** out, long long outer, int C,
     p->param_type = param_type;
     p->eps = (float)eps;
     for (long long& s : p->stride) s = C * inner;
-    p->forward = norm_choose(outer, C, inner, type, false, -1);
-    p->backward = norm_choose(outer, C, inner, type, true, -1);
+    for (int s = 0; s < kNormStages; ++s) p->shape[s] = norm_choose(outer, C, inner, type, (NormStage)s, -1);
     *out = p;
     return DWM_OK;
 }
@@ -251,9 +255,13 @@ dwm_status_t dwm_norm_set_variant(dwm_norm_plan_t* plan, const char* stage, int 
     const bool backward = !std::strcmp(stage, "backward");
     if (!backward && std::strcmp(stage, "forward")) return DWM_ERR_INVALID_ARG;
     if (backward && plan->ws) return DWM_ERR_WORKSPACE;
-    const NormShape s = norm_choose(plan->outer, plan->C, plan->inner, plan->type, backward, variant);
-    if (s.kernel < 0) return DWM_ERR_INVALID_ARG;
-    (backward ? plan->backward : plan->forward) = s;
+    const int from = backward ? kNormBackward : kNormForward, to = backward ? kNormStages : kNormBackward;
+    NormShape asked[kNormStages];
+    for (int s = from; s < to; ++s) {
+        asked[s] = norm_choose(plan->outer, plan->C, plan->inner, plan->type, (NormStage)s, variant);
+        if (asked[s].kernel < 0) return DWM_ERR_INVALID_ARG;
+    }
+    std::memcpy(plan->shape + from, asked + from, (to - from) * sizeof(NormShape));
     return DWM_OK;
 }
 
@@ -263,15 +271,16 @@ dwm_status_t dwm_norm_plan_info(const dwm_norm_plan_t* plan, dwm_norm_info_t* in
     info->outer = plan->outer;
     info->C = plan->C;
     info->inner = plan->inner;
-    info->forward_kernel = plan->forward.kernel;
-    info->backward_kernel = plan->backward.kernel;
-    info->splits = plan->backward.blocks;
+    info->forward_kernel = plan->shape[dwm::kNormForward].kernel;
+    info->join_forward_kernel = plan->shape[dwm::kNormJoinForward].kernel;
+    info->backward_kernel = plan->shape[dwm::kNormBackward].kernel;
+    info->splits = plan->shape[dwm::kNormBackward].blocks;
     return DWM_OK;
 }
 
 size_t dwm_norm_workspace_bytes(const dwm_norm_plan_t* plan)
 {
-    return plan ? (size_t)plan->backward.blocks * 2 * plan->C * sizeof(float) : 0;
+    return plan ? (size_t)plan->shape[dwm::kNormBackward].blocks * 2 * plan->C * sizeof(float) : 0;
 }
 
 dwm_status_t dwm_norm_set_workspace(dwm_norm_plan_t* plan, void* ws_dev, size_t bytes)
@@ -289,7 +298,7 @@ dwm_status_t dwm_norm_forward(const dwm_norm_plan_t* plan, const void* x_dev, co
     if (!plan || !given(*plan, {x_dev, y_dev})) return DWM_ERR_INVALID_ARG;
     if (!tensors_ok(*plan, {x_dev, y_dev}) || !params_ok(*plan, {gamma_dev, beta_dev}) || !stats_ok(mean_dev, rstd_dev))
         return DWM_ERR_INVALID_ARG;
-    NormArgs a = args_of(*plan, plan->forward);
+    NormArgs a = args_of(*plan);
     a.x = x_dev;
     a.gamma = gamma_dev;
     a.beta = beta_dev;
@@ -309,7 +318,7 @@ dwm_status_t dwm_norm_backward(const dwm_norm_plan_t* plan, const void* dy_dev, 
     if (!tensors_ok(*plan, {dy_dev, x_dev, dx_dev}) || !params_ok(*plan, {gamma_dev, dgamma_dev, dbeta_dev}) ||
         !stats_ok(mean_dev, rstd_dev))
         return DWM_ERR_INVALID_ARG;
-    NormArgs a = args_of(*plan, plan->backward);
+    NormArgs a = args_of(*plan);
     a.dy = dy_dev;
     a.z = const_cast<void*>(x_dev);
     a.stride[kNormZ] = plan->stride[kNormX];
@@ -332,7 +341,7 @@ dwm_status_t dwm_norm_join_forward(const dwm_norm_plan_t* plan, const dwm_dropou
     if (!tensors_ok(*plan, {x_dev, residual_dev, z_dev, y_dev}) || !params_ok(*plan, {gamma_dev, beta_dev}) ||
         !stats_ok(mean_dev, rstd_dev))
         return DWM_ERR_INVALID_ARG;
-    NormArgs a = args_of(*plan, plan->forward);
+    NormArgs a = args_of(*plan);
     if (!drop_args(drop, &a.drop)) return DWM_ERR_INVALID_ARG;
     a.x = x_dev;
     a.residual = residual_dev;
@@ -357,7 +366,7 @@ dwm_status_t dwm_norm_join_backward(const dwm_norm_plan_t* plan, const dwm_dropo
     if (!tensors_ok(*plan, {dy_dev, dz_dev, z_dev, dx_dev, dresidual_dev}) ||
         !params_ok(*plan, {gamma_dev, dgamma_dev, dbeta_dev}) || !stats_ok(mean_dev, rstd_dev))
         return DWM_ERR_INVALID_ARG;
-    NormArgs a = args_of(*plan, plan->backward);
+    NormArgs a = args_of(*plan);
     if (!drop_args(drop, &a.drop)) return DWM_ERR_INVALID_ARG;
     a.dy = dy_dev;
     a.dz = dz_dev;

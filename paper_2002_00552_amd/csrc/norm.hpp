@@ -111,7 +111,8 @@ struct NormShape {
 };
 
 // The planner's choice (variant < 0), or the kernel asked for; kernel = -1: it does not apply.
-NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, bool backward, int variant);
+enum NormStage { kNormForward, kNormJoinForward, kNormBackward, kNormStages };
+NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, NormStage stage, int variant);
 
 dwm_status_t launch_norm_any_forward(const NormArgs& a, dwm_type_t type, bool join, void* stream);
 dwm_status_t launch_norm_any_backward(const NormArgs& a, dwm_type_t type, void* stream);
@@ -129,6 +130,6 @@ struct dwm_norm_plan {
     dwm_type_t type, param_type;
     float eps;
     long long stride[dwm::kNormTensors];
-    dwm::NormShape forward, backward;
+    dwm::NormShape shape[dwm::kNormStages];
     void* ws;
 };
