@@ -53,7 +53,8 @@ static int rows_choice(long long outer, int C, int vec, bool backward)
 // Backward in binary32 eight do not pay (64 images of 256, 28 x 28: 39.4, 45.9), with 16 bits from twice the size on (64 of 96, 55 x 55: 39.1, 33.8;
 // of 128, 28 x 28: 15.5, 16.4).  In the forward pass over 129 to 256 channels and in both over 17 to 32 eight always do (64 images of
 // 256, 14 x 14, bfloat16: 8.3, 7.7; of 32, 112 x 112, binary32: 48, 44 and 71, 69).  A join, which holds the residual and the draws too, does not over
-// more than 256 (64 images of 512, 14 x 14, binary32: 30.4, 40.5; of 1024: 67, 75), except with 16 bits over more than 512 (48.4, 41.7).
+// more than 256 (64 images of 512, 14 x 14, binary32: 30.4, 40.5; 300 of 700, 5 x 5, binary16: 32.2, 47.2; of 4 x 7 26.1, 38.3; the other way round 64 of 1024,
+// 14 x 14, bfloat16: 48.4, 41.7).
 static int maps_choice(int C, int size, long long vectors, bool one, NormStage stage)
 {
     const bool backward = stage == kNormBackward;
@@ -64,7 +65,7 @@ static int maps_choice(int C, int size, long long vectors, bool one, NormStage s
     const NormMaps &m = kNormMaps[eight], &n = kNormMaps[four];
     if (m.cg == 4) return C > 16 ? eight : four;
     if (m.cg * m.k > n.cg * n.k) return four;  // (made for more channels)
-    if (stage == kNormJoinForward && C > 256 && (size == 4 || C <= 512)) return four;
+    if (stage == kNormJoinForward && C > 256) return four;
     const long long threads = maps_tiles(eight, vectors) * m.pl * m.cg, enough = 256 * 768;
     return (m.cg == 32 && C > 128) || threads >= (backward ? 2 : 1) * enough ? eight : four;
 }
