@@ -47,27 +47,31 @@ static int rows_choice(long long outer, int C, int vec, bool backward)
     return -1;
 }
 
-// Maps: four channels a thread, so that a tile is small and many are under way, or, where tiles of eight channels a thread are still enough
-// for the chip, those, whose lanes lie along more pixels.  us, four and eight, forward: 64 images of 1024 channels, 14 x 14, binary32: 35.3,
-// 30.0; of 7 x 7: 12.3, 13.9; 64 of 512, 14 x 14, binary32: 18.0, 15.6; 8 images of 96, 55 x 55, bfloat16: 6.3, 6.8; 64 of them: 22.0, 20.7.
-// Backward in binary32 eight do not pay (64 images of 256, 28 x 28: 39.4, 45.9), with 16 bits from twice the size on (64 of 96, 55 x 55: 39.1, 33.8;
-// of 128, 28 x 28: 15.5, 16.4).  In the forward pass over 129 to 256 channels and in both over 17 to 32 eight always do (64 images of
-// 256, 14 x 14, bfloat16: 8.3, 7.7; of 32, 112 x 112, binary32: 48, 44 and 71, 69).  A join, which holds the residual and the draws too, does not over
-// more than 256 (64 images of 512, 14 x 14, binary32: 30.4, 40.5; 300 of 700, 5 x 5, binary16: 32.2, 47.2; of 4 x 7 26.1, 38.3; the other way round 64 of 1024,
-// 14 x 14, bfloat16: 48.4, 41.7).
+// Maps: four channels a thread, so that a tile is small and many are under way, or, where wider tiles (six or eight channels a thread, whose lanes lie
+// along more pixels) are still enough for the chip, those.  us, four and wide, forward: 64 images of 1024 channels, 14 x 14, binary32: 35.5,
+// 31.8; of 7 x 7: 13.3, 15.7; 8 images of 512, 20 x 20, binary16: 6.1, 7.0; 64 of 300: 15.3, 13.2; 64 of 96, 55 x 55, bfloat16: 26.6, 23.2; 8 of them:
+// 6.3, 6.8.  Tiles of 1024 threads have to be twice as many (300 images of 700, 5 x 5, binary32: 20.7, 22.6).  Over 129 to 256 channels and over 17 to
+// 32 they always pay (32 images of 192, 28 x 28, bfloat16: 9.7, 8.1; 64 of 32, 112 x 112, binary32: 48, 44).
+// Backward in binary32 wide tiles do not pay (64 images of 256, 28 x 28: 39.4, 45.9), with 16 bits from twice the size on (64 of 96, 55 x 55: 40.2,
+// 35.4; 64 of 300, 20 x 20, a join: 35.4, 33.1; of 128, 28 x 28: 17.9, 18.8).
+// A join holds the residual and the draws too.  With 16 bits wide tiles pay as for a norm (64 images of 300, 20 x 20: 25.1, 23.6; of 512, 14 x 14: 23.2, 22.0;
+// of 1024: 46.4, 38.7), but not with eight channels over 193 to 256 (16 of 256, 14 x 14: 7.6, 8.7; 64 of them, 28 x 28: 29.9, 31.7); in binary32 with six,
+// or eight up to 128, from three times the size on (10 of 259, 88 x 82: 74.2, 70.9; 64 of 300, 20 x 20: 34.2, 35.3; 64 of 96, 55 x 55: 78.8, 73.8;
+// of 128, 28 x 28: 24.9, 28.1), else not (64 of 1024, 14 x 14: 67.4, 74.7).
 static int maps_choice(int C, int size, long long vectors, bool one, NormStage stage)
 {
     const bool backward = stage == kNormBackward;
-    int four = -1, eight = -1;
+    int four = -1, wide = -1;
     for (int i = kNormMapsShapes - 1; i >= 0; --i)
-        if (maps_fit(i, C, size, one, backward)) (kNormMaps[i].k == 4 ? four : eight) = i;
-    if (four < 0 || eight < 0) return four < 0 ? eight : four;
-    const NormMaps &m = kNormMaps[eight], &n = kNormMaps[four];
-    if (m.cg == 4) return C > 16 ? eight : four;
+        if (maps_fit(i, C, size, one, backward)) (kNormMaps[i].k == 4 ? four : wide) = i;
+    if (four < 0 || wide < 0) return four < 0 ? wide : four;
+    const NormMaps &m = kNormMaps[wide], &n = kNormMaps[four];
+    if (m.cg == 4) return C > 16 ? wide : four;
     if (m.cg * m.k > n.cg * n.k) return four;  // (made for more channels)
-    if (stage == kNormJoinForward && C > 256) return four;
-    const long long threads = maps_tiles(eight, vectors) * m.pl * m.cg, enough = 256 * 768;
-    return (m.cg == 32 && C > 128) || threads >= (backward ? 2 : 1) * enough ? eight : four;
+    const bool join = stage == kNormJoinForward;
+    if (join && m.k == 8 && (m.cg == 32 || (size == 4 && m.cg > 32))) return four;
+    const long long threads = maps_tiles(wide, vectors) * m.pl * m.cg, enough = 256 * 768;
+    return (m.cg == 32 && C > 128 && !join) || threads >= (backward || m.cg == 128 ? 2 : join && size == 4 ? 3 : 1) * enough ? wide : four;
 }
 
 // How many workgroups: forward, enough to fill the chip several times over; backward over maps, two for each of the 256 CUs, since each writes its

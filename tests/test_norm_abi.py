@@ -139,7 +139,7 @@ def test_dropouts_that_are_refused():
 def test_variants_that_do_not_apply():
     rows, maps = dwm.dwm_norm_plan_create(8, 600, 1, dwm.DWM_F32, dwm.DWM_F32, 1e-5), dwm.dwm_norm_plan_create(8, 600, 7, dwm.DWM_BF16, dwm.DWM_F32, 1e-5)
     try:
-        for plan, good, bad in ((rows, (0, 8, 13, -1), (1, 4, 14, 100, 204, 99)), (maps, (0, 109, 111, 209, 211, -1), (1, 107, 207, 210, 212, 300, 100))):
+        for plan, good, bad in ((rows, (0, 8, 13, -1), (1, 4, 14, 100, 204, 99)), (maps, (0, 111, 112, 113, 211, 213, -1), (1, 110, 210, 212, 214, 300, 100))):
             for stage in ("forward", "backward"):
                 for v in good:
                     dwm.dwm_norm_set_variant(plan, stage, v)
