@@ -6,12 +6,6 @@
 
 namespace dwm {
 
-template <class T> __device__ __forceinline__ float param(const void* p, int typed, long long c, float none)
-{
-    if (!p) return none;
-    return typed ? (float)((const T*)p)[c] : ((const float*)p)[c];
-}
-
 // K parameters, `step` channels apart from channel c on, and behind the last channel that one.  The kinds part in front of the loads, so
 // that these go out together (64 images of 96 channels, 55 x 55, parameters in binary16: 27.9 us with a load after the other, 24.6).
 template <class T, int K> __device__ __forceinline__ void strided_params(const void* p, int typed, int c, int step, int C, float none, float (&f)[K])
