@@ -83,7 +83,7 @@ __global__ __launch_bounds__(256) void norm_any_forward_kernel(NormArgs a)
             }
         });
         const T* vp = JOIN ? zp : xp;
-        const float m0 = position_sum<L>(sum, lds) * inv_c;
+        const float m0 = rounded_product(position_sum<L>(sum, lds), inv_c);
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll 4
         for (int c = g; c < n; c += G) {
