@@ -74,11 +74,12 @@ template <int N> __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 
-// Sums over the lanes of a wave that are N apart, 2 N apart, ...: for all of them.
+// Sums over the lanes of a wave that are N apart, 2 N apart, ...: for all of them, and the same number for all, which takes eight lanes in front of
+// four (four first: two lanes eight apart add the pairs that they are in, two lanes four apart others).
 template <int N> __device__ __forceinline__ float strided_sum(float v)
 {
-    if (N <= 4) v += dpp<0x124>(v);  // four lanes on, round in sixteen
-    if (N <= 8) v += dpp<0x128>(v);  // eight
+    if (N <= 8) v += dpp<0x128>(v);  // eight lanes on, round in sixteen
+    if (N <= 4) v += dpp<0x124>(v);  // four
     if (N <= 16) v = add_across<16>(v);
     if (N <= 32) v = add_across<32>(v);
     return v;

@@ -17,7 +17,7 @@ import paper_2002_00552_amd as dwm
 pytestmark = pytest.mark.gpu
 
 TYPE = {"f32": dwm.DWM_F32, "f16": dwm.DWM_F16, "bf16": dwm.DWM_BF16}
-KERNELS = [*range(0, 14), *(v for v in [*range(100, 114), *range(200, 214)] if v % 100 not in (8, 11, 13))]  # dwm_norm_set_variant's numbers
+KERNELS = [-1, *range(0, 14), *range(100, 114), *range(200, 214)]  # dwm_norm_set_variant's numbers
 U = ref.U
 # 32 elements of a thread, 6 steps over a wave and 4 over the waves; maps 8, 4 and 16; kernels for any size, at the sizes here: rows 47
 # and 8 (12001 channels), maps 47 and 5 (1500 channels, 32 threads a pixel)
@@ -122,5 +122,5 @@ def test_means_far_above_the_deviations(shape, dtype):
                         _within(out.double().cpu().numpy(), want, which)
                     except AssertionError as e:
                         wrong.append("%s: %s" % (what, str(e).split("\n")[0]))
-    assert taken >= 1
+    assert taken >= 3
     assert not wrong, "%d\n" % len(wrong) + "\n".join(wrong[:12])
