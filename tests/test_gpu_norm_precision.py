@@ -1,5 +1,5 @@
 """Norms whose mean is far above their deviations, through every kernel: rows and pixels of one value, of one value but for one element, and
-of a few neighbouring values, against 64 bits.
+of a few neighbouring values, in each storage type, against 64 bits.
 
 What is allowed follows from the kernels' own way, not from the number of channels alone.  With c the longest path of additions that an
 element takes (CHAIN), the first mean m0 is off by `first` = c U mean|z| + U max|z| at most.  Deviations from it are exact or off by U
@@ -93,7 +93,7 @@ MAPS = [(2, 56, 50), (1, 96, 49), (2, 224, 33), (2, 300, 50), (1, 500, 40), (1, 
 BASE = {"f32": (300.1, 12345.678), "f16": (644.0, 3000.0), "bf16": (644.0, 10304.0)}
 
 
-@pytest.mark.parametrize("dtype", ["f32"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("shape", ROWS + MAPS, ids=lambda s: "x".join(map(str, s)))
 def test_means_far_above_the_deviations(shape, dtype):
     outer, C, inner = shape
