@@ -124,3 +124,39 @@ def test_means_far_above_the_deviations(shape, dtype):
                         wrong.append("%s: %s" % (what, str(e).split("\n")[0]))
     assert taken >= 3
     assert not wrong, "%d\n" % len(wrong) + "\n".join(wrong[:12])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 60, 1), (2, 3000, 1), (2, 40, 49), (3, 300, 50), (1, 1024, 36), (1, 1500, 8), (1, 2100, 9)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_gradients_of_norms_of_tiny_values(shape, dtype):
+    """Values of 1e-20 and eps = 0, so rstd is 1e20: its square is beyond binary32, the gradient is not.  Bounds of norm_reference.py."""
+    outer, C, inner = shape
+    rng = np.random.default_rng(23)
+    x, dy = (ref.rounded(s * rng.standard_normal(shape), dtype).cuda() for s in (1e-20, 1e-3))
+    gamma32 = (1 + 0.5 * rng.standard_normal(C)).astype(np.float32)
+    gamma = torch.from_numpy(gamma32).cuda()
+    z, dy64, g64 = x.double().cpu().numpy(), dy.double().cpu().numpy(), gamma32.astype(np.float64)
+    mean, rstd = (torch.from_numpy(a.astype(np.float32)).cuda() for a in ref.norm(z, g64, np.zeros(C), 0.0)[1:])
+    m, r = mean.double().cpu().numpy(), rstd.double().cpu().numpy()
+    want = ref.norm_backward(dy64, z, g64, m, r)
+    allowed = ref.tolerances_backward(dy64, z, g64, m, r, np.zeros(shape), want[0], dtype, "f32", want[1], want[2])
+    taken = 0
+    for variant in KERNELS:
+        plan = dwm.dwm_norm_plan_create(*shape, TYPE[dtype], dwm.DWM_F32, 0.0)
+        try:
+            dwm.dwm_norm_set_variant(plan, "backward", variant)
+            ws = torch.empty(max(dwm.dwm_norm_workspace_bytes(plan), 256), dtype=torch.uint8, device="cuda")
+            dwm.dwm_norm_set_workspace(plan, ws.data_ptr(), ws.numel())
+            taken += 1
+            dx, dgamma, dbeta = torch.full_like(x, float("nan")), torch.full_like(gamma, float("nan")), torch.full_like(gamma, float("nan"))
+            args = (gamma.data_ptr(), mean.data_ptr(), rstd.data_ptr(), dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), _stream())
+            dwm.dwm_norm_backward(plan, dy.data_ptr(), x.data_ptr(), *args)
+            for got, w, t, name in zip((dx, dgamma, dbeta), want, allowed, ("dx", "dgamma", "dbeta")):
+                _within(got.double().cpu().numpy(), (w, t), "kernel %d: %s" % (variant, name))
+        except dwm.DwmError as e:
+            assert e.status == dwm.DWM_ERR_INVALID_ARG
+        finally:
+            torch.cuda.synchronize()
+            dwm.dwm_norm_plan_destroy(plan)
+    assert taken >= 2
