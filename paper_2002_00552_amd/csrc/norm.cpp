@@ -195,7 +195,9 @@ static dwm_status_t run_backward(const dwm_norm_plan& p, const NormArgs& a, bool
     if (!params || p.shape[kNormBackward].aside) b.partial = nullptr;
     if (params && p.shape[kNormBackward].aside) {
         b.aside = 1;
-        if (a.dy == a.dx || a.dy == a.dresidual) {  // dy would be overwritten while it is read: the parameters' gradients first
+        if (!a.dx && !a.dresidual) {  // nothing else to make
+            b.splits = 0;
+        } else if (a.dy == a.dx || a.dy == a.dresidual) {  // dy would be overwritten while it is read: the parameters' gradients first
             b.splits = 0;
             const dwm_status_t st = run_kernel(p, b, p.shape[kNormBackward], true, join, stream);
             if (st != DWM_OK) return st;
