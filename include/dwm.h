@@ -507,7 +507,8 @@ DWM_API dwm_status_t dwm_norm_set_stride(dwm_norm_plan_t* plan, const char* tens
 /* A kernel by number, for tuning and tests: stage "forward" or "backward" (this one before dwm_norm_set_workspace only,
  * DWM_ERR_WORKSPACE afterwards); 0 = the kernels for any size; rows (inner = 1): 1 .. 13, the library's internal table of threads of a row
  * and vectors of a thread; maps: 100 .. 113 with four pixels a lane, 200 .. 213 with one; negative: the planner's
- * choice.  DWM_ERR_INVALID_ARG for one that cannot hold C channels or is not built in that direction.  All give the same results up to the order of sums. */
+ * choice.  DWM_ERR_INVALID_ARG for one that cannot hold C channels or is not built in that direction; one that is not built for joins leaves
+ * those to the planner.  All give the same results up to the order of sums. */
 DWM_API dwm_status_t dwm_norm_set_variant(dwm_norm_plan_t* plan, const char* stage, int variant);
 /* The workspace holds partial sums of dgamma and dbeta: 256-byte aligned, needed by backward calls that are asked for one of
  * them and by no other call. */

@@ -27,11 +27,11 @@ static bool rows_fit(int shape, int C, int vec, bool backward)
     const int holds = r.tpr * r.k * vec;
     return holds >= C && C >= vec && (backward ? r.backward && holds <= kNormRowsWidest : r.forward);
 }
-static bool maps_fit(int shape, int C, int size, bool one, bool backward)
+static bool maps_fit(int shape, int C, int size, bool one, NormStage stage)
 {
     if (shape < 0 || shape >= kNormMapsShapes) return false;
     const NormMaps& m = kNormMaps[shape];
-    return m.cg * m.k >= C && (!one || m.one) && (!backward || size <= m.backward);
+    return m.cg * m.k >= C && (!one || m.one) && (stage != kNormJoinForward || size <= m.join) && (stage != kNormBackward || size <= m.backward);
 }
 static long long maps_tiles(int shape, long long vectors) { return (vectors + kNormMaps[shape].pl - 1) / kNormMaps[shape].pl; }
 
@@ -55,21 +55,19 @@ static int rows_choice(long long outer, int C, int vec, bool backward)
 // Backward in binary32 wide tiles do not pay (64 images of 256, 28 x 28: 39.4, 45.9), with 16 bits from twice the size on (64 of 96, 55 x 55: 40.2,
 // 35.4; 64 of 300, 20 x 20, a join: 35.4, 33.1; of 128, 28 x 28: 17.9, 18.8).
 // A join holds the residual and the draws too.  With 16 bits wide tiles pay as for a norm (64 images of 300, 20 x 20: 25.1, 23.6; of 512, 14 x 14: 23.2, 22.0;
-// of 1024: 46.4, 38.7), but not with eight channels over 193 to 256 (16 of 256, 14 x 14: 7.6, 8.7; 64 of them, 28 x 28: 29.9, 31.7); in binary32 with six,
+// of 1024: 46.4, 38.7), but not with eight channels over 193 to 256 (16 of 256, 14 x 14: 7.6, 8.7; 64 of them, 28 x 28: 29.9, 31.7: not built); in binary32 with six,
 // or eight up to 128, from three times the size on (10 of 259, 88 x 82: 74.2, 70.9; 64 of 300, 20 x 20: 34.2, 35.3; 64 of 96, 55 x 55: 78.8, 73.8;
-// of 128, 28 x 28: 24.9, 28.1), else not (64 of 1024, 14 x 14: 67.4, 74.7).
+// of 128, 28 x 28: 24.9, 28.1), else not (64 of 1024, 14 x 14: 67.4, 74.7: not built).
 static int maps_choice(int C, int size, long long vectors, bool one, NormStage stage)
 {
-    const bool backward = stage == kNormBackward;
+    const bool backward = stage == kNormBackward, join = stage == kNormJoinForward;
     int four = -1, wide = -1;
     for (int i = kNormMapsShapes - 1; i >= 0; --i)
-        if (maps_fit(i, C, size, one, backward)) (kNormMaps[i].k == 4 ? four : wide) = i;
+        if (maps_fit(i, C, size, one, stage)) (kNormMaps[i].k == 4 ? four : wide) = i;
     if (four < 0 || wide < 0) return four < 0 ? wide : four;
     const NormMaps &m = kNormMaps[wide], &n = kNormMaps[four];
     if (m.cg == 4) return C > 16 ? wide : four;
     if (m.cg * m.k > n.cg * n.k) return four;  // (made for more channels)
-    const bool join = stage == kNormJoinForward;
-    if (join && m.k == 8 && (m.cg == 32 || (size == 4 && m.cg > 32))) return four;
     const long long threads = maps_tiles(wide, vectors) * m.pl * m.cg, enough = 256 * 768;
     return (m.cg == 32 && C > 128 && !join) || threads >= (backward || m.cg == 128 ? 2 : join && size == 4 ? 3 : 1) * enough ? wide : four;
 }
@@ -101,7 +99,7 @@ NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, 
     const bool one = variant < 0 ? inner < kNormMapsPixels || positions * C <= 1 << 20 : variant >= kNormMapsOne;
     const long long vectors = one ? positions : outer * ((inner + kNormMapsPixels - 1) / kNormMapsPixels), limit = (1LL << 31) - 64;  // (indexes in 32 bits)
     const int shape = variant < 0 ? maps_choice(C, size, vectors, one, stage) : variant - (one ? kNormMapsOne : kNormMapsVec);
-    if (!maps_fit(shape, C, size, one, backward) || !(one || inner >= kNormMapsPixels) || vectors >= limit || inner >= limit)
+    if (!maps_fit(shape, C, size, one, stage) || !(one || inner >= kNormMapsPixels) || vectors >= limit || inner >= limit)
         return variant < 0 ? any : none;
     return {(one ? kNormMapsOne : kNormMapsVec) + shape, workgroups(maps_tiles(shape, vectors), backward ? kMapsBackwardBlocks : kForwardBlocks), small && positions <= 4096};
 }
@@ -266,6 +264,8 @@ dwm_status_t dwm_norm_set_variant(dwm_norm_plan_t* plan, const char* stage, int 
     NormShape asked[kNormStages];
     for (int s = from; s < to; ++s) {
         asked[s] = norm_choose(plan->outer, plan->C, plan->inner, plan->type, (NormStage)s, variant);
+        if (s == kNormJoinForward && asked[s].kernel < 0)  // (a shape of the plain norm alone)
+            asked[s] = norm_choose(plan->outer, plan->C, plan->inner, plan->type, kNormJoinForward, -1);
         if (asked[s].kernel < 0) return DWM_ERR_INVALID_ARG;
     }
     std::memcpy(plan->shape + from, asked + from, (to - from) * sizeof(NormShape));

@@ -46,16 +46,16 @@ struct NormRows {
 };
 struct NormMaps {
     int pl, cg, k;
-    bool one;       // with one pixel a lane too
-    int backward;   // the largest element size of a backward kernel
+    bool one;            // with one pixel a lane too
+    int join, backward;  // the largest element size of a join's forward kernel and of a backward one (0: none)
 };
 constexpr NormRows kNormRows[] = {
     {8, 1, true, true},    {16, 1, true, true},   {32, 1, true, true},   {64, 1, true, true},   {64, 2, true, false},  {128, 1, true, true},   {128, 2, true, false},
     {256, 1, true, true},  {256, 2, true, false}, {512, 1, true, true},  {512, 2, true, true},  {1024, 2, true, true}, {1024, 4, true, true},
 };
 constexpr NormMaps kNormMaps[] = {
-    {64, 4, 4, true, 4},  {64, 4, 8, false, 4}, {16, 16, 4, true, 4}, {8, 32, 4, true, 4},  {16, 16, 8, false, 2}, {8, 32, 6, false, 0},  {8, 32, 8, false, 0},
-    {8, 64, 4, true, 4},  {4, 128, 4, true, 4}, {8, 64, 6, false, 2}, {8, 64, 8, false, 2}, {4, 256, 4, true, 4},  {8, 128, 8, false, 2}, {4, 256, 8, true, 4},
+    {64, 4, 4, true, 4, 4}, {64, 4, 8, false, 4, 4}, {16, 16, 4, true, 4, 4}, {8, 32, 4, true, 4, 4},  {16, 16, 8, false, 4, 2}, {8, 32, 6, false, 4, 0},  {8, 32, 8, false, 0, 0},
+    {8, 64, 4, true, 4, 4}, {4, 128, 4, true, 4, 4}, {8, 64, 6, false, 4, 2}, {8, 64, 8, false, 2, 2}, {4, 256, 4, true, 4, 4},  {8, 128, 8, false, 2, 2}, {4, 256, 8, true, 4, 4},
 };
 constexpr int kNormRowsShapes = sizeof(kNormRows) / sizeof(kNormRows[0]), kNormMapsShapes = sizeof(kNormMaps) / sizeof(kNormMaps[0]);
 

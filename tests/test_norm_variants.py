@@ -1,0 +1,46 @@
+"""Kernels of the layer norms by number: a join takes the number that is asked for where it is built and the planner's elsewhere, and the planner's
+numbers are all among those that can be asked for; no GPU is needed."""
+import pytest
+
+import paper_2002_00552_amd as dwm
+
+NUMBERS = [*range(0, 14), *range(100, 114), *range(200, 214)]
+
+
+def _kernels(plan):
+    info = dwm.dwm_norm_plan_info(plan)
+    return info.forward_kernel, info.join_forward_kernel, info.backward_kernel
+
+
+@pytest.mark.parametrize("type, C, number, joins", [
+    (dwm.DWM_F32, 256, 106, False), (dwm.DWM_F16, 256, 106, False), (dwm.DWM_BF16, 200, 106, False), (dwm.DWM_F32, 512, 110, False),
+    (dwm.DWM_F32, 1000, 112, False), (dwm.DWM_F16, 512, 110, True), (dwm.DWM_BF16, 1000, 112, True), (dwm.DWM_F32, 384, 109, True)])
+def test_joins_without_a_kernel_of_their_own_number(type, C, number, joins):
+    plan = dwm.dwm_norm_plan_create(64, C, 400, type, dwm.DWM_F32, 1e-5)
+    try:
+        _, chosen, _ = _kernels(plan)
+        dwm.dwm_norm_set_variant(plan, "forward", number)
+        assert _kernels(plan)[:2] == (number, number if joins else chosen)
+        assert chosen != number or joins
+    finally:
+        dwm.dwm_norm_plan_destroy(plan)
+
+
+@pytest.mark.parametrize("type", [dwm.DWM_F32, dwm.DWM_F16, dwm.DWM_BF16])
+def test_the_planner_chooses_what_can_be_asked_for(type):
+    for outer in (1, 7, 64, 3000, 70000):
+        for inner in (1, 2, 4, 49, 784):
+            for C in (1, 3, 8, 17, 40, 64, 100, 129, 200, 256, 300, 500, 512, 600, 1000, 1500, 2048, 2049, 5000, 16384, 16392, 40000):
+                if outer * inner * C > 1 << 40:
+                    continue
+                plan = dwm.dwm_norm_plan_create(outer, C, inner, type, dwm.DWM_F32, 1e-5)
+                try:
+                    forward, join, backward = _kernels(plan)
+                    assert {forward, join, backward} <= set(NUMBERS)
+                    for stage, number, which in (("forward", forward, 0), ("forward", join, 1), ("backward", backward, 2)):
+                        dwm.dwm_norm_set_variant(plan, stage, number)
+                        assert _kernels(plan)[which] == number
+                        dwm.dwm_norm_set_variant(plan, stage, -1)
+                    assert _kernels(plan) == (forward, join, backward)
+                finally:
+                    dwm.dwm_norm_plan_destroy(plan)
