@@ -39,8 +39,16 @@ static long long maps_tiles(int shape, long long vectors) { return (vectors + kN
 // (2048 rows of 4096 bfloat16: 9.4 us with two vectors, 9.9 with one; 256 rows of 2048: 3.8 and 3.6).  Backward: one vector a
 // thread wherever there is a shape for it (4096 rows of 1500 bfloat16: 21.7 us with two, 17.5 with one; 65536 of 1024: 83 and 81; 16384 of 2048: 44
 // both).
-static int rows_choice(long long outer, int C, int vec, bool backward)
+// Forward, 16385 to 32768 channels of 16 bits: the shape that holds them spills registers, and is taken for a row on each CU (two of a bfloat16 norm's, four
+// of a binary16 one's: it spills least); with more rows the kernel for any size, which reads them again, is ahead.  us, in registers and any size, rows of 24576,
+// parameters in binary32: joins of 256 rows 41, 52, of 320 71, 61, of 2000 292, 178; norms in bfloat16 of 512 rows 35, 36, of 1024 62, 46; in binary16
+// of 1024 44, 47, of 4000 170, 156.
+static long long spilling_rows(dwm_type_t type, NormStage stage) { return stage == kNormJoinForward ? 256 : type == DWM_BF16 ? 512 : 1024; }
+static int rows_choice(long long outer, int C, dwm_type_t type, NormStage stage)
 {
+    const bool backward = stage == kNormBackward;
+    const int vec = type == DWM_F32 ? 4 : 8;
+    if (C > kNormRowsWidest && outer > spilling_rows(type, stage)) return -1;
     for (int pass = backward || outer < 2048 ? 0 : 1; pass < 2; ++pass)
         for (int i = 0; i < kNormRowsShapes; ++i)
             if (rows_fit(i, C, vec, backward) && (pass == 1 || kNormRows[i].k == 1)) return i;
@@ -88,7 +96,7 @@ NormShape norm_choose(long long outer, int C, long long inner, dwm_type_t type, 
     const bool small = positions * C * size <= 8 << 20;
     // (rows shorter than a vector are taken as maps of one pixel)
     if (inner == 1 && (variant < 0 ? C >= 16 / size : variant < kNormMapsVec)) {
-        const int vec = 16 / size, shape = variant < 0 ? rows_choice(outer, C, vec, backward) : variant - kNormRowsFirst;
+        const int vec = 16 / size, shape = variant < 0 ? rows_choice(outer, C, type, stage) : variant - kNormRowsFirst;
         if (!rows_fit(shape, C, vec, backward)) return variant < 0 ? any : none;
         const int tpr = kNormRows[shape].tpr, threads = backward ? norm_rows_threads(kNormRows[shape], C % vec != 0) : tpr > 256 ? tpr : 256;
         const long long blocks = (outer + threads / tpr - 1) / (threads / tpr);

@@ -44,3 +44,21 @@ def test_the_planner_chooses_what_can_be_asked_for(type):
                     assert _kernels(plan) == (forward, join, backward)
                 finally:
                     dwm.dwm_norm_plan_destroy(plan)
+
+
+@pytest.mark.parametrize("type, rows, join_rows", [(dwm.DWM_F16, 1024, 256), (dwm.DWM_BF16, 512, 256)])
+@pytest.mark.parametrize("C", [16385, 20001, 32768])
+def test_rows_that_spill_registers_are_few(type, rows, join_rows, C):
+    """Shape 13 holds 16-bit rows of more than 16384 channels in more registers than there are: with many rows the kernel for any size is ahead."""
+    for outer in (1, join_rows, join_rows + 1, rows, rows + 1, 100000):
+        plan = dwm.dwm_norm_plan_create(outer, C, 1, type, dwm.DWM_F32, 1e-5)
+        try:
+            assert _kernels(plan) == (13 if outer <= rows else 0, 13 if outer <= join_rows else 0, 0)
+        finally:
+            dwm.dwm_norm_plan_destroy(plan)
+    for kind, most in ((dwm.DWM_F32, 16384), (type, 16384)):  # no spills up to there
+        plan = dwm.dwm_norm_plan_create(100000, most, 1, kind, dwm.DWM_F32, 1e-5)
+        try:
+            assert 0 not in _kernels(plan)
+        finally:
+            dwm.dwm_norm_plan_destroy(plan)
