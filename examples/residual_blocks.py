@@ -110,9 +110,9 @@ class Blocks:
                                        self.dh.data_ptr(), self.dz.data_ptr(), self.dgamma[k].data_ptr(), self.dbeta[k].data_ptr(), _stream())
             self.conv.backward(self.y[l], self.w[l], self.dh, self.dy, self.dw[l])
         # the first norm reads x, which is the stream's start too: a join without a branch
-        dwm.dwm_norm_join_backward(self.norm, None, self.dy.data_ptr(), self.dz.data_ptr(), self.z[0].data_ptr(), self.gamma[0].data_ptr(),
-                                   self.mean[0].data_ptr(), self.rstd[0].data_ptr(), None, self.dx.data_ptr(), self.dgamma[0].data_ptr(),
-                                   self.dbeta[0].data_ptr(), _stream())
+        dwm.dwm_norm_join_backward(self.norm, None, self.dy.data_ptr(), self.dz.data_ptr() if self.blocks else None, self.z[0].data_ptr(),
+                                   self.gamma[0].data_ptr(), self.mean[0].data_ptr(), self.rstd[0].data_ptr(), None, self.dx.data_ptr(),
+                                   self.dgamma[0].data_ptr(), self.dbeta[0].data_ptr(), _stream())
         return self.dx
 
     def descend(self, rate):
