@@ -468,7 +468,7 @@ typedef enum { DWM_F32 = 0, DWM_F16 = 1, DWM_BF16 = 2 } dwm_type_t;
 
 /* Which elements are dropped, and without a mask in memory: element e of a tensor in its dense order ((o*C + c)*inner + i,
  * whatever the strides) takes word e % 4 of the block that Philox-4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, SC 2011)
- * makes of the counter (e / 4, sequence) under the key seed, and is dropped where that word is below p * 2^32.  The backward call
+ * makes of the counter (e / 4, sequence) under the key seed, and is dropped where that word is below p * 2^32, rounded to a whole number.  The backward call
  * takes the same values and draws the same mask.  Masks of different (seed, sequence) are independent: a program counts sequence
  * up from call to call, or, where calls are replayed from a graph, the number at sequence_dev (added to sequence when the
  * kernel runs).  A kept element is multiplied by 1 / (1 - p), rounded to binary32; a dropped one becomes zero whatever it

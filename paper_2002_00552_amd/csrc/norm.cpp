@@ -41,7 +41,7 @@ static long long maps_tiles(int shape, long long vectors) { return (vectors + kN
 // both).
 // Forward, 16385 to 32768 channels of 16 bits: the shape that holds them spills registers, and is taken for a row on each CU (two of a bfloat16 norm's, four
 // of a binary16 one's: it spills least); with more rows the kernel for any size, which reads them again, is ahead.  us, in registers and any size, rows of 24576,
-// parameters in binary32: joins of 256 rows 41, 52, of 320 71, 61, of 2000 292, 178; norms in bfloat16 of 512 rows 35, 36, of 1024 62, 46; in binary16
+// parameters in binary32: joins of 256 rows 40, 52, of 320 71, 61, of 2000 292, 178; norms in bfloat16 of 512 rows 35, 36, of 1024 62, 46; in binary16
 // of 1024 44, 47, of 4000 170, 156.
 static long long spilling_rows(dwm_type_t type, NormStage stage) { return stage == kNormJoinForward ? 256 : type == DWM_BF16 ? 512 : 1024; }
 static int rows_choice(long long outer, int C, dwm_type_t type, NormStage stage)
