@@ -464,7 +464,12 @@ DWM_API dwm_status_t dwm_bf16_contract_output(const dwm_bf16_plan_t* plan, const
  * stream.  Outputs overlap nothing, except that an output may be the very memory, with the same stride, of one input: y of x in
  * dwm_norm_forward and dwm_dropout_forward, z of residual, dx of dy, dresidual of dz.  Results do not vary from run to run.
  */
-typedef enum { DWM_F32 = 0, DWM_F16 = 1, DWM_BF16 = 2 } dwm_type_t;
+typedef enum {
+    DWM_F32 = 0,
+    DWM_F16 = 1,
+    DWM_BF16 = 2,
+    DWM_PACKED = 3 /* rows in 8 bits (dwm_packed_t): operands of dwm_matmul_packed alone; every other call refuses it */
+} dwm_type_t;
 
 /* Which elements are dropped, and without a mask in memory: element e of a tensor in its dense order ((o*C + c)*inner + i,
  * whatever the strides) takes word e % 4 of the block that Philox-4x32 with ten rounds (Salmon, Moraes, Dror, Shaw, SC 2011)
@@ -538,6 +543,151 @@ DWM_API dwm_status_t dwm_norm_join_backward(const dwm_norm_plan_t* plan, const d
                                             const void* dz_dev, const void* z_dev, const void* gamma_dev,
                                             const float* mean_dev, const float* rstd_dev, void* dx_dev, void* dresidual_dev,
                                             void* dgamma_dev, void* dbeta_dev, void* stream);
+
+/*
+ * The pointwise branch of a residual block, over rows (tokens, pooled features, pixels with their channels last): rows in 8 bits,
+ * root-mean-square norms with the residual's addition, activations with checkpoints in 8 bits, matrix products with an epilogue.
+ * Tensors are [rows][C] with a stride between rows; memory, streams and errors as for the layer norms above: plans are host
+ * memory, everything else is the caller's device memory at multiples of its element's size, nothing is allocated or synchronised,
+ * kernels go to `stream`, which belongs to the current device, as the memory does, calls can be captured into a HIP graph.  Calls that use the same
+ * plan's workspace must be ordered on one stream; calls that use none may run at once.  Results do not vary from run to run.
+ * Outputs overlap nothing, except that an output may be the very memory, with the same stride and type, of one input where that is said.
+ *
+ * Rows in 8 bits ("packed").  Each row is cut into blocks of 32 channels, the last one filled up with zeros.  A block has a scale
+ * byte s: the smallest whose 448 * 2^(s - 127) is not below the block's largest finite magnitude; 0 where that is zero.  An element v is
+ * the e4m3 code (OCP 8-bit floating point: 4 bits of exponent, 3 of mantissa, up to 448, no infinities) nearest to
+ * v / 2^(s - 127), ties to even; infinities and NaN become a NaN of their own and change no other element.  It stands for
+ * code * 2^(s - 127).  codes: [rows][32 * ceil(C / 32)] bytes, at a multiple of 16; scales: [rows][4 * ceil(C / 128)]
+ * bytes, at a multiple of 4, those behind the last block zero.  Calls that read packed rows take zeros behind the last channel and
+ * the last block for granted.  8.25 bits a value where C is a multiple of 128.
+ */
+typedef struct {
+    void* codes;  /* device memory */
+    void* scales; /* device memory */
+} dwm_packed_t;
+
+/* 0 where rows < 0, C < 1 or dwm_pack would refuse them as unsupported. */
+DWM_API size_t dwm_packed_codes_bytes(long long rows, int C);
+DWM_API size_t dwm_packed_scales_bytes(long long rows, int C);
+/* rows >= 0 (0: nothing to do), C >= 1, stride >= C elements.  DWM_ERR_UNSUPPORTED for C above 2^20, more than 2^40 elements (rows
+ * times stride too).  dwm_unpack rounds once to `type` (a binary16 too large becomes an infinity). */
+DWM_API dwm_status_t dwm_pack(dwm_type_t type, long long rows, int C, const void* x_dev, long long stride,
+                              const dwm_packed_t* packed, void* stream);
+DWM_API dwm_status_t dwm_unpack(dwm_type_t type, long long rows, int C, const dwm_packed_t* packed, void* y_dev, long long stride,
+                                void* stream);
+
+/*
+ * Root-mean-square norm, with the addition of a residual in front of it:
+ *     z = residual + x (rounded to binary32, then to its type), rstd = 1 / sqrt((1/C) sum_c z^2 + eps), y = z * rstd * gamma[c]
+ * the norm reads z as it is stored.  Values of up to about 1e19 / sqrt(C) can be normed; an infinity or NaN spoils its own row alone.
+ */
+typedef struct dwm_rms_plan dwm_rms_plan_t;
+typedef struct {
+    long long rows;
+    int C;
+    int forward_kernel, backward_kernel; /* dwm_rms_set_variant's numbers */
+    int splits;                          /* parts of the rows whose sums of dgamma are added up last */
+} dwm_rms_info_t;
+
+/* rows >= 0 (0: calls write no tensor; dgamma becomes zero), C >= 1, eps >= 0 and finite; param_type is DWM_F32 or type.
+ * DWM_ERR_UNSUPPORTED for C above 2^20 or more than 2^40 elements.  Host only. */
+DWM_API dwm_status_t dwm_rms_plan_create(dwm_rms_plan_t** out, long long rows, int C, dwm_type_t type, dwm_type_t param_type,
+                                         double eps);
+DWM_API dwm_status_t dwm_rms_plan_destroy(dwm_rms_plan_t* plan);
+DWM_API dwm_status_t dwm_rms_plan_info(const dwm_rms_plan_t* plan, dwm_rms_info_t* info);
+/* Elements between one row and the next of "x", "residual", "z", "y", "dy", "dz" or "dx": at least C, the default.  At any time. */
+DWM_API dwm_status_t dwm_rms_set_stride(dwm_rms_plan_t* plan, const char* tensor, long long stride);
+/* A kernel by number, for tuning and tests: stage "forward" or "backward" (this one before dwm_rms_set_workspace only,
+ * DWM_ERR_WORKSPACE afterwards); 0 = any size, 1 .. 14 = the library's internal table of threads of a row and octets of a thread,
+ * negative: the planner's choice.  DWM_ERR_INVALID_ARG for one that does not hold C channels or is not built. */
+DWM_API dwm_status_t dwm_rms_set_variant(dwm_rms_plan_t* plan, const char* stage, int variant);
+/* The workspace holds partial sums of dgamma: 256-byte aligned, needed by backward calls that are asked for it and by no other. */
+DWM_API size_t dwm_rms_workspace_bytes(const dwm_rms_plan_t* plan);
+DWM_API dwm_status_t dwm_rms_set_workspace(dwm_rms_plan_t* plan, void* ws_dev, size_t bytes);
+/* residual NULL: z is x, and z_dev has to be NULL.  gamma may be NULL (ones); any of z, y, y_packed (y in 8 bits, from binary32),
+ * kept (z in 8 bits, as it is stored) and rstd ([rows]) may be NULL, but not all of them.  z may be residual or x, y may be x. */
+DWM_API dwm_status_t dwm_rms_forward(const dwm_rms_plan_t* plan, const void* x_dev, const void* residual_dev, const void* gamma_dev,
+                                     void* z_dev, void* y_dev, const dwm_packed_t* y_packed, const dwm_packed_t* kept,
+                                     float* rstd_dev, void* stream);
+/* From z or from kept (one of the two, the other NULL; the values that kept stands for take the place of z, rstd is that of the
+ * forward pass), with xhat = z * rstd and g = dy * gamma:
+ *     dx = dz + rstd * (g - xhat * (1/C) sum_c g*xhat),   dgamma = sum over the rows of dy * xhat
+ * dx is the gradient of x and of residual; dz (NULL: none) is what reaches z from elsewhere.  dx or dgamma may be NULL, not both.
+ * dx may be dy or dz. */
+DWM_API dwm_status_t dwm_rms_backward(const dwm_rms_plan_t* plan, const void* dy_dev, const void* dz_dev, const void* z_dev,
+                                      const dwm_packed_t* kept, const void* gamma_dev, const float* rstd_dev, void* dx_dev,
+                                      void* dgamma_dev, void* stream);
+
+/*
+ * Activations with a bias, and with what their gradient needs kept in 8 bits:
+ *     p = x + bias[c] (rounded to binary32),  y = act(p),  dx = dy * act'(p),  dbias = sum over the rows of dx (before it is rounded)
+ * relu: max(p, 0), with a gradient of 0 at 0; gelu: p (1 + erf(p / sqrt 2)) / 2; silu: p / (1 + exp(-p)).  NaN stays NaN in all;
+ * at an infinity gelu and silu and their gradients may be NaN.
+ */
+typedef enum { DWM_ACT_NONE = 0, DWM_ACT_RELU = 1, DWM_ACT_GELU = 2, DWM_ACT_SILU = 3 } dwm_act_t;
+typedef struct dwm_act_plan dwm_act_plan_t;
+
+/* Limits as for dwm_rms_plan_create; rows = 0: dbias becomes zero. */
+DWM_API dwm_status_t dwm_act_plan_create(dwm_act_plan_t** out, dwm_act_t act, long long rows, int C, dwm_type_t type,
+                                         dwm_type_t param_type);
+DWM_API dwm_status_t dwm_act_plan_destroy(dwm_act_plan_t* plan);
+/* "x", "y", "dy" or "dx". */
+DWM_API dwm_status_t dwm_act_set_stride(dwm_act_plan_t* plan, const char* tensor, long long stride);
+/* Partial sums of dbias: 256-byte aligned, needed by backward calls that are asked for it and by no other. */
+DWM_API size_t dwm_act_workspace_bytes(const dwm_act_plan_t* plan);
+DWM_API dwm_status_t dwm_act_set_workspace(dwm_act_plan_t* plan, void* ws_dev, size_t bytes);
+/* bias may be NULL; y or kept (p in 8 bits) may be NULL, not both.  y may be x. */
+DWM_API dwm_status_t dwm_act_forward(const dwm_act_plan_t* plan, const void* x_dev, const void* bias_dev, void* y_dev,
+                                     const dwm_packed_t* kept, void* stream);
+/* From kept (x and bias NULL), or from x and bias (kept NULL; bias may be NULL).  dx or dbias may be NULL, not both.  dx may be dy
+ * or x.  With DWM_ACT_NONE x and kept may both be NULL: dbias is then the sum of dy's rows. */
+DWM_API dwm_status_t dwm_act_backward(const dwm_act_plan_t* plan, const void* dy_dev, const void* x_dev, const void* bias_dev,
+                                      const dwm_packed_t* kept, void* dx_dev, void* dbias_dev, void* stream);
+
+/*
+ * Matrix products with an epilogue:
+ *     p[m][n] = sum_k a[m][k] * b[n][k] + bias[n],   out[m][n] = act(p) + residual[m][n]
+ * with sums in binary32 and one rounding.  The same call makes the products of the backward pass: with dp the gradient of p,
+ * da = dp b is the product of dp and of b with its contraction axis across its rows (DWM_B_ACROSS), db = dp^T a that of both
+ * across (DWM_A_ACROSS | DWM_B_ACROSS), dbias and dp come from dwm_act_backward and kept.
+ */
+enum {
+    DWM_A_ACROSS = 1, /* a is [K][M] (element (m, k) at k * stride + m), not [M][K] */
+    DWM_B_ACROSS = 2  /* b is [K][N], not [N][K] */
+};
+typedef struct dwm_matmul_plan dwm_matmul_plan_t;
+typedef struct {
+    int M, N, K;
+    int kernel; /* dwm_matmul_set_variant's numbers: what runs where the operands are aligned */
+    int splits; /* parts of K whose products are added up last */
+} dwm_matmul_info_t;
+
+/* operands: DWM_F16 or DWM_BF16, with type (that of out and residual) the same or DWM_F32; or DWM_PACKED, with type DWM_F16 or
+ * DWM_BF16 and flags 0.  param_type (of bias) is DWM_F32 or the 16-bit one of the two types.  M, N >= 0 (0: nothing to do), K >= 0 (0: p = bias).  DWM_ERR_UNSUPPORTED for M, N or K above
+ * 2^24, M * N above 2^37, or other types.  Host only. */
+DWM_API dwm_status_t dwm_matmul_plan_create(dwm_matmul_plan_t** out, int M, int N, int K, dwm_type_t operands, dwm_type_t type,
+                                            dwm_type_t param_type, dwm_act_t act, int flags);
+DWM_API dwm_status_t dwm_matmul_plan_destroy(dwm_matmul_plan_t* plan);
+DWM_API dwm_status_t dwm_matmul_plan_info(const dwm_matmul_plan_t* plan, dwm_matmul_info_t* info);
+/* Elements between rows of "a", "b" (16-bit operands), "residual" or "out".  At any time.  16-bit operands whose address is a multiple of 16 and
+ * whose stride and row length are multiples of 8 take the faster kernels. */
+DWM_API dwm_status_t dwm_matmul_set_stride(dwm_matmul_plan_t* plan, const char* tensor, long long stride);
+/* For tuning and tests, before dwm_matmul_set_workspace only (DWM_ERR_WORKSPACE afterwards): "kernel": 0 = any alignment (not built for
+ * packed operands), 1 = tiles of 128 x 128, 2 = 256 x 256, 3 = few rows (M <= 64, neither operand across); "splits": 1 .. 64; negative: the planner's
+ * choice.  DWM_ERR_INVALID_ARG for what does not apply. */
+DWM_API dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, int variant);
+/* Sums of the parts of K: 256-byte aligned; 0 bytes: not needed. */
+DWM_API size_t dwm_matmul_workspace_bytes(const dwm_matmul_plan_t* plan);
+DWM_API dwm_status_t dwm_matmul_set_workspace(dwm_matmul_plan_t* plan, void* ws_dev, size_t bytes);
+/* 16-bit operands.  bias and residual may be NULL; any of out, y_packed (act(p) + residual in 8 bits, from binary32) and kept (p in 8
+ * bits, from binary32) may be NULL, but not all of them.  out may be residual (sums of gradients). */
+DWM_API dwm_status_t dwm_matmul(const dwm_matmul_plan_t* plan, const void* a_dev, const void* b_dev, const void* bias_dev,
+                                const void* residual_dev, void* out_dev, const dwm_packed_t* y_packed, const dwm_packed_t* kept,
+                                void* stream);
+/* The same with a [M][K] and b [N][K] packed (dwm_pack, y_packed of a norm or of another product). */
+DWM_API dwm_status_t dwm_matmul_packed(const dwm_matmul_plan_t* plan, const dwm_packed_t* a, const dwm_packed_t* b,
+                                       const void* bias_dev, const void* residual_dev, void* out_dev, const dwm_packed_t* y_packed,
+                                       const dwm_packed_t* kept, void* stream);
 
 DWM_API const char* dwm_status_string(dwm_status_t status);
 

@@ -64,7 +64,9 @@ class dwm_bwd_filter_info_t(ctypes.Structure):
                 ("direct_flops", ctypes.c_double), ("winograd_flops", ctypes.c_double)]
 
 
-DWM_F32, DWM_F16, DWM_BF16 = range(3)
+DWM_F32, DWM_F16, DWM_BF16, DWM_PACKED = range(4)
+DWM_ACT_NONE, DWM_ACT_RELU, DWM_ACT_GELU, DWM_ACT_SILU = range(4)
+DWM_A_ACROSS, DWM_B_ACROSS = 1, 2
 
 
 class dwm_dropout_t(ctypes.Structure):
@@ -78,10 +80,23 @@ class dwm_norm_info_t(ctypes.Structure):
                 ("splits", ctypes.c_int)]
 
 
+class dwm_packed_t(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
+
+
+class dwm_rms_info_t(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_longlong)] + [(n, ctypes.c_int) for n in ("C", "forward_kernel", "backward_kernel", "splits")]
+
+
+class dwm_matmul_info_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("M", "N", "K", "kernel", "splits")]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _L = ctypes.c_longlong
 _DROP = ctypes.POINTER(dwm_dropout_t)
+_PACKED = ctypes.POINTER(dwm_packed_t)
 _SIGNATURES = {
     "dwm_plan_create": (_I, [ctypes.POINTER(_P)] + [_I] * 9),
     "dwm_plan_destroy": (_I, [_P]),
@@ -161,6 +176,35 @@ _SIGNATURES = {
     "dwm_norm_backward": (_I, [_P] * 10),
     "dwm_norm_join_forward": (_I, [_P, _DROP] + [_P] * 9),
     "dwm_norm_join_backward": (_I, [_P, _DROP] + [_P] * 11),
+    "dwm_packed_codes_bytes": (ctypes.c_size_t, [_L, _I]),
+    "dwm_packed_scales_bytes": (ctypes.c_size_t, [_L, _I]),
+    "dwm_pack": (_I, [_I, _L, _I, _P, _L, _PACKED, _P]),
+    "dwm_unpack": (_I, [_I, _L, _I, _PACKED, _P, _L, _P]),
+    "dwm_rms_plan_create": (_I, [ctypes.POINTER(_P), _L, _I, _I, _I, ctypes.c_double]),
+    "dwm_rms_plan_destroy": (_I, [_P]),
+    "dwm_rms_plan_info": (_I, [_P, ctypes.POINTER(dwm_rms_info_t)]),
+    "dwm_rms_set_stride": (_I, [_P, ctypes.c_char_p, _L]),
+    "dwm_rms_set_variant": (_I, [_P, ctypes.c_char_p, _I]),
+    "dwm_rms_workspace_bytes": (ctypes.c_size_t, [_P]),
+    "dwm_rms_set_workspace": (_I, [_P, _P, ctypes.c_size_t]),
+    "dwm_rms_forward": (_I, [_P] * 6 + [_PACKED] * 2 + [_P] * 2),
+    "dwm_rms_backward": (_I, [_P] * 4 + [_PACKED] + [_P] * 5),
+    "dwm_act_plan_create": (_I, [ctypes.POINTER(_P), _I, _L, _I, _I, _I]),
+    "dwm_act_plan_destroy": (_I, [_P]),
+    "dwm_act_set_stride": (_I, [_P, ctypes.c_char_p, _L]),
+    "dwm_act_workspace_bytes": (ctypes.c_size_t, [_P]),
+    "dwm_act_set_workspace": (_I, [_P, _P, ctypes.c_size_t]),
+    "dwm_act_forward": (_I, [_P] * 4 + [_PACKED, _P]),
+    "dwm_act_backward": (_I, [_P] * 4 + [_PACKED] + [_P] * 3),
+    "dwm_matmul_plan_create": (_I, [ctypes.POINTER(_P)] + [_I] * 8),
+    "dwm_matmul_plan_destroy": (_I, [_P]),
+    "dwm_matmul_plan_info": (_I, [_P, ctypes.POINTER(dwm_matmul_info_t)]),
+    "dwm_matmul_set_stride": (_I, [_P, ctypes.c_char_p, _L]),
+    "dwm_matmul_set_variant": (_I, [_P, ctypes.c_char_p, _I]),
+    "dwm_matmul_workspace_bytes": (ctypes.c_size_t, [_P]),
+    "dwm_matmul_set_workspace": (_I, [_P, _P, ctypes.c_size_t]),
+    "dwm_matmul": (_I, [_P] * 6 + [_PACKED] * 2 + [_P]),
+    "dwm_matmul_packed": (_I, [_P] + [_PACKED] * 2 + [_P] * 3 + [_PACKED] * 2 + [_P]),
 }
 EXPORTS = sorted(_SIGNATURES)
 
@@ -539,3 +583,131 @@ def dwm_norm_join_backward(plan, drop, dy_dev, dz_dev, z_dev, gamma_dev, mean_de
                            dbeta_dev, stream=None):
     _check(lib().dwm_norm_join_backward(plan, drop, dy_dev, dz_dev, z_dev, gamma_dev, mean_dev, rstd_dev, dx_dev, dresidual_dev,
                                         dgamma_dev, dbeta_dev, stream), "dwm_norm_join_backward")
+
+
+def dwm_packed_codes_bytes(rows, C):
+    return int(lib().dwm_packed_codes_bytes(rows, C))
+
+
+def dwm_packed_scales_bytes(rows, C):
+    return int(lib().dwm_packed_scales_bytes(rows, C))
+
+
+def dwm_pack(type, rows, C, x_dev, stride, packed, stream=None):
+    _check(lib().dwm_pack(type, rows, C, x_dev, stride, packed, stream), "dwm_pack")
+
+
+def dwm_unpack(type, rows, C, packed, y_dev, stride, stream=None):
+    _check(lib().dwm_unpack(type, rows, C, packed, y_dev, stride, stream), "dwm_unpack")
+
+
+def dwm_rms_plan_create(rows, C, type, param_type, eps):
+    h = _P()
+    _check(lib().dwm_rms_plan_create(ctypes.byref(h), rows, C, type, param_type, eps), "dwm_rms_plan_create")
+    return h
+
+
+def dwm_rms_plan_destroy(plan):
+    _check(lib().dwm_rms_plan_destroy(plan), "dwm_rms_plan_destroy")
+
+
+def dwm_rms_plan_info(plan):
+    info = dwm_rms_info_t()
+    _check(lib().dwm_rms_plan_info(plan, ctypes.byref(info)), "dwm_rms_plan_info")
+    return info
+
+
+def dwm_rms_set_stride(plan, tensor, stride):
+    _check(lib().dwm_rms_set_stride(plan, tensor.encode(), stride), "dwm_rms_set_stride(%s)" % tensor)
+
+
+def dwm_rms_set_variant(plan, stage, variant):
+    _check(lib().dwm_rms_set_variant(plan, stage.encode(), variant), "dwm_rms_set_variant(%s)" % stage)
+
+
+def dwm_rms_workspace_bytes(plan):
+    return int(lib().dwm_rms_workspace_bytes(plan))
+
+
+def dwm_rms_set_workspace(plan, ws_dev, nbytes):
+    _check(lib().dwm_rms_set_workspace(plan, ws_dev, nbytes), "dwm_rms_set_workspace")
+
+
+def dwm_rms_forward(plan, x_dev, residual_dev, gamma_dev, z_dev, y_dev, y_packed=None, kept=None, rstd_dev=None, stream=None):
+    _check(lib().dwm_rms_forward(plan, x_dev, residual_dev, gamma_dev, z_dev, y_dev, y_packed, kept, rstd_dev, stream),
+           "dwm_rms_forward")
+
+
+def dwm_rms_backward(plan, dy_dev, dz_dev, z_dev, kept, gamma_dev, rstd_dev, dx_dev, dgamma_dev, stream=None):
+    _check(lib().dwm_rms_backward(plan, dy_dev, dz_dev, z_dev, kept, gamma_dev, rstd_dev, dx_dev, dgamma_dev, stream),
+           "dwm_rms_backward")
+
+
+def dwm_act_plan_create(act, rows, C, type, param_type):
+    h = _P()
+    _check(lib().dwm_act_plan_create(ctypes.byref(h), act, rows, C, type, param_type), "dwm_act_plan_create")
+    return h
+
+
+def dwm_act_plan_destroy(plan):
+    _check(lib().dwm_act_plan_destroy(plan), "dwm_act_plan_destroy")
+
+
+def dwm_act_set_stride(plan, tensor, stride):
+    _check(lib().dwm_act_set_stride(plan, tensor.encode(), stride), "dwm_act_set_stride(%s)" % tensor)
+
+
+def dwm_act_workspace_bytes(plan):
+    return int(lib().dwm_act_workspace_bytes(plan))
+
+
+def dwm_act_set_workspace(plan, ws_dev, nbytes):
+    _check(lib().dwm_act_set_workspace(plan, ws_dev, nbytes), "dwm_act_set_workspace")
+
+
+def dwm_act_forward(plan, x_dev, bias_dev, y_dev, kept=None, stream=None):
+    _check(lib().dwm_act_forward(plan, x_dev, bias_dev, y_dev, kept, stream), "dwm_act_forward")
+
+
+def dwm_act_backward(plan, dy_dev, x_dev, bias_dev, kept, dx_dev, dbias_dev, stream=None):
+    _check(lib().dwm_act_backward(plan, dy_dev, x_dev, bias_dev, kept, dx_dev, dbias_dev, stream), "dwm_act_backward")
+
+
+def dwm_matmul_plan_create(M, N, K, operands, type, param_type, act=DWM_ACT_NONE, flags=0):
+    h = _P()
+    _check(lib().dwm_matmul_plan_create(ctypes.byref(h), M, N, K, operands, type, param_type, act, flags), "dwm_matmul_plan_create")
+    return h
+
+
+def dwm_matmul_plan_destroy(plan):
+    _check(lib().dwm_matmul_plan_destroy(plan), "dwm_matmul_plan_destroy")
+
+
+def dwm_matmul_plan_info(plan):
+    info = dwm_matmul_info_t()
+    _check(lib().dwm_matmul_plan_info(plan, ctypes.byref(info)), "dwm_matmul_plan_info")
+    return info
+
+
+def dwm_matmul_set_stride(plan, tensor, stride):
+    _check(lib().dwm_matmul_set_stride(plan, tensor.encode(), stride), "dwm_matmul_set_stride(%s)" % tensor)
+
+
+def dwm_matmul_set_variant(plan, stage, variant):
+    _check(lib().dwm_matmul_set_variant(plan, stage.encode(), variant), "dwm_matmul_set_variant(%s)" % stage)
+
+
+def dwm_matmul_workspace_bytes(plan):
+    return int(lib().dwm_matmul_workspace_bytes(plan))
+
+
+def dwm_matmul_set_workspace(plan, ws_dev, nbytes):
+    _check(lib().dwm_matmul_set_workspace(plan, ws_dev, nbytes), "dwm_matmul_set_workspace")
+
+
+def dwm_matmul(plan, a_dev, b_dev, bias_dev, residual_dev, out_dev, y_packed=None, kept=None, stream=None):
+    _check(lib().dwm_matmul(plan, a_dev, b_dev, bias_dev, residual_dev, out_dev, y_packed, kept, stream), "dwm_matmul")
+
+
+def dwm_matmul_packed(plan, a, b, bias_dev, residual_dev, out_dev, y_packed=None, kept=None, stream=None):
+    _check(lib().dwm_matmul_packed(plan, a, b, bias_dev, residual_dev, out_dev, y_packed, kept, stream), "dwm_matmul_packed")

@@ -15,7 +15,8 @@ LIB = os.path.join(HERE, "libdwm.so")
 SOURCES = ["plan.cpp", "setup.cpp", "transforms.hip", "contract.hip", "contract_split.hip", "fused.hip", "direct.hip", "wgrad_direct.hip",
            "contract_batch.hip",
            "backward.hip", "backward_small.hip", "wgrad.hip", "wgrad_split.hip", "half.hip", "bf16.hip", "noalloc.hip",
-           "norm.cpp", "norm_any.hip", "norm_f32.hip", "norm_f16.hip", "norm_bf16.hip", "dropout.hip"]
+           "norm.cpp", "norm_any.hip", "norm_f32.hip", "norm_f16.hip", "norm_bf16.hip", "dropout.hip",
+           "branch.cpp", "rms.hip", "act.hip", "matmul_f16.hip", "matmul_bf16.hip", "matmul_packed.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

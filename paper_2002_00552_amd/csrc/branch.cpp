@@ -1,0 +1,522 @@
+// The pointwise branch over rows: plans, checks of arguments and entry points (host only, plain C++).
+#include "branch.hpp"
+
+#include <cstring>
+#include <new>
+
+namespace dwm {
+namespace {
+
+size_t size_of(dwm_type_t type) { return type == DWM_F32 ? 4 : 2; }
+bool known(dwm_type_t type) { return type == DWM_F32 || type == DWM_F16 || type == DWM_BF16; }
+bool known(dwm_act_t act) { return act >= DWM_ACT_NONE && act <= DWM_ACT_SILU; }
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+bool rows_fit(long long rows, long long C) { return C <= kMostChannels && rows <= kMostElements / C; }
+
+// Packed rows that a call is given: there in whole, and where they have to lie.
+bool packed_ok(const dwm_packed_t* p) { return !p || (p->codes && p->scales && aligned(p->codes, 16) && aligned(p->scales, 4)); }
+Packed packed_of(const dwm_packed_t* p) { return p ? Packed{(uint8_t*)p->codes, (uint8_t*)p->scales} : Packed{nullptr, nullptr}; }
+
+template <int N> int named(const char* const (&names)[N], const char* name)
+{
+    for (int i = 0; name && i < N; ++i)
+        if (!std::strcmp(name, names[i])) return i;
+    return -1;
+}
+
+bool rms_fits(int variant, int C, bool backward)
+{
+    if (variant < 1 || variant > kRmsShapeCount) return variant == 0;
+    const RmsShape& s = kRmsShapes[variant - 1];
+    return s.tpr * s.k * kOctet >= C && (backward ? s.backward : s.forward);
+}
+
+// The narrowest shape that holds a row: one octet a thread where rows are few, two from 2048 on.
+int rms_choice(long long rows, int C, bool backward)
+{
+    for (int pass = rows < 2048 ? 0 : 1; pass < 2; ++pass)
+        for (int v = 1; v <= kRmsShapeCount; ++v)
+            if (rms_fits(v, C, backward) && (pass == 1 || kRmsShapes[v - 1].k == 1)) return v;
+    return 0;
+}
+
+int rms_splits(long long rows, int C, int kernel)
+{
+    if (kernel == 0) {
+        const long long groups = (C + 2047) / 2048, most = groups > 1024 ? 1 : 1024 / groups, some = (rows + 31) / 32;
+        return (int)(some < 1 ? 1 : some < most ? some : most);
+    }
+    const int tpr = kRmsShapes[kernel - 1].tpr, threads = tpr > 256 ? tpr : 256;
+    const long long blocks = (rows + threads / tpr - 1) / (threads / tpr), most = 256 * 1024 / threads;
+    return (int)(blocks < 1 ? 1 : blocks < most ? blocks : most);
+}
+
+int act_splits(long long rows, int C)
+{
+    const long long groups = (C + 2047) / 2048, most = groups > 1024 ? 1 : 1024 / groups;
+    long long lanes = 1;
+    while (lanes < 256 && lanes * kOctet < C) lanes *= 2;
+    const long long some = (rows + 4 * (256 / lanes) - 1) / (4 * (256 / lanes));
+    return (int)(some < 1 ? 1 : some < most ? some : most);
+}
+
+// Tiles of a kernel, the steps of K they go through, and how the parts of K are chosen: as many as fill the 256 CUs, each of some steps.
+int matmul_splits(const dwm_matmul_plan& p, int kernel)
+{
+    const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step;
+    const long long side = kernel == kMat256 ? 256 : 128;
+    const long long tiles = ((p.M + side - 1) / side) * ((p.N + side - 1) / side), fill = kernel == kMat256 ? 256 : 512;
+    if (tiles == 0 || kernel == kMatFew) return 1;
+    long long splits = fill / tiles;
+    if (splits > steps / 4) splits = steps / 4;
+    if (splits > 16) splits = 16;
+    return (int)(splits < 1 ? 1 : splits);
+}
+
+bool matmul_applies(const dwm_matmul_plan& p, int kernel)
+{
+    if (kernel == kMatFew) return false;
+    return kernel == kMatAny ? p.operands != DWM_PACKED : kernel == kMat128 || kernel == kMat256;
+}
+
+int matmul_choice(const dwm_matmul_plan& p) { return p.operands == DWM_PACKED ? kMat128 : kMatAny; }
+
+void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
+{
+    p.shape.kernel = kernel;
+    p.shape.splits = splits > 0 ? splits : matmul_splits(p, kernel);
+    p.any.kernel = p.operands == DWM_PACKED || kernel == kMatFew ? kernel : kMatAny;
+    p.any.splits = splits > 0 ? splits : matmul_splits(p, p.any.kernel);
+}
+
+// Whether the kernels that copy sixteen bytes at a time straight into LDS can read an operand.
+bool operand_aligned(const void* p, long long stride, long long length) { return aligned(p, 16) && stride % 8 == 0 && length % 8 == 0; }
+
+dwm_status_t run_matmul(const dwm_matmul_plan& p, MatmulArgs& a, const MatmulShape& shape, const void* bias, const void* residual,
+                        void* out, const dwm_packed_t* packed_y, const dwm_packed_t* kept, void* stream)
+{
+    if (shape.splits > 1 && !p.ws) return DWM_ERR_WORKSPACE;
+    std::memcpy(a.stride, p.stride, sizeof(a.stride));
+    a.bias = bias;
+    a.residual = residual;
+    a.out = out;
+    a.packed_y = packed_of(packed_y);
+    a.kept = packed_of(kept);
+    a.partial = (float*)p.ws;
+    a.M = p.M;
+    a.N = p.N;
+    a.K = p.K;
+    a.splits = shape.splits;
+    a.act = p.act;
+    a.param_typed = p.param_type != DWM_F32;
+    a.wide_out = p.type == DWM_F32;
+    a.bf16_out = p.type == DWM_BF16;
+    switch (p.operands) {
+        case DWM_F16: return launch_matmul_f16(a, p.flags, shape.kernel, stream);
+        case DWM_BF16: return launch_matmul_bf16(a, p.flags, shape.kernel, stream);
+        case DWM_PACKED: return launch_matmul_packed(a, p.flags, shape.kernel, stream);
+        default: return DWM_ERR_INVALID_ARG;
+    }
+}
+
+// What both matmul calls ask of everything but the operands.
+bool matmul_ok(const dwm_matmul_plan& p, const void* bias, const void* residual, const void* out, const dwm_packed_t* packed_y,
+               const dwm_packed_t* kept)
+{
+    return (out || packed_y || kept || p.M == 0 || p.N == 0) && aligned(bias, size_of(p.param_type)) && aligned(residual, size_of(p.type)) &&
+           aligned(out, size_of(p.type)) && packed_ok(packed_y) && packed_ok(kept);
+}
+
+const char* const kRmsNames[kRmsTensors] = {"x", "residual", "z", "y", "dy", "dz", "dx"};
+const char* const kActNames[kActTensors] = {"x", "y", "dy", "dx"};
+const char* const kMatNames[kMatTensors] = {"a", "b", "residual", "out"};
+
+}  // namespace
+}  // namespace dwm
+
+using namespace dwm;
+
+extern "C" {
+
+size_t dwm_packed_codes_bytes(long long rows, int C)
+{
+    return rows < 0 || C < 1 || !rows_fit(rows, C) ? 0 : (size_t)(rows * packed_width(C));
+}
+
+size_t dwm_packed_scales_bytes(long long rows, int C)
+{
+    return rows < 0 || C < 1 || !rows_fit(rows, C) ? 0 : (size_t)(rows * packed_scales(C));
+}
+
+static dwm_status_t pack_args(ActArgs* a, dwm_type_t type, long long rows, int C, const void* tensor, long long stride,
+                              const dwm_packed_t* packed)
+{
+    if (!known(type) || rows < 0 || C < 1 || stride < C || (rows > 0 && (!tensor || !packed)) || !packed_ok(packed) || !aligned(tensor, size_of(type)))
+        return DWM_ERR_INVALID_ARG;
+    if (!rows_fit(rows, C) || (rows > 0 && stride > kMostElements / rows)) return DWM_ERR_UNSUPPORTED;
+    *a = ActArgs{};
+    a->rows = rows;
+    a->C = C;
+    a->kept = packed_of(packed);
+    for (long long& s : a->stride) s = stride;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_pack(dwm_type_t type, long long rows, int C, const void* x_dev, long long stride, const dwm_packed_t* packed, void* stream)
+{
+    ActArgs a;
+    const dwm_status_t st = pack_args(&a, type, rows, C, x_dev, stride, packed);
+    if (st != DWM_OK || rows == 0) return st;
+    a.x = x_dev;
+    return launch_act_forward(a, type, stream);
+}
+
+dwm_status_t dwm_unpack(dwm_type_t type, long long rows, int C, const dwm_packed_t* packed, void* y_dev, long long stride, void* stream)
+{
+    ActArgs a;
+    const dwm_status_t st = pack_args(&a, type, rows, C, y_dev, stride, packed);
+    if (st != DWM_OK || rows == 0) return st;
+    a.y = y_dev;
+    return launch_act_forward(a, type, stream);
+}
+
+dwm_status_t dwm_rms_plan_create(dwm_rms_plan_t** out, long long rows, int C, dwm_type_t type, dwm_type_t param_type, double eps)
+{
+    if (!out || rows < 0 || C < 1 || !known(type) || !(param_type == DWM_F32 || param_type == type) || !(eps >= 0.0) || !(eps <= 3e38))
+        return DWM_ERR_INVALID_ARG;
+    if (!rows_fit(rows, C)) return DWM_ERR_UNSUPPORTED;
+    dwm_rms_plan* p = new (std::nothrow) dwm_rms_plan;
+    if (!p) return DWM_ERR_ALLOC;
+    std::memset(p, 0, sizeof(*p));
+    p->rows = rows;
+    p->C = C;
+    p->type = type;
+    p->param_type = param_type;
+    p->eps = (float)eps;
+    for (long long& s : p->stride) s = C;
+    p->forward = rms_choice(rows, C, false);
+    p->backward = rms_choice(rows, C, true);
+    p->splits = rms_splits(rows, C, p->backward);
+    *out = p;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_rms_plan_destroy(dwm_rms_plan_t* plan)
+{
+    if (!plan) return DWM_ERR_INVALID_ARG;
+    delete plan;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_rms_plan_info(const dwm_rms_plan_t* plan, dwm_rms_info_t* info)
+{
+    if (!plan || !info) return DWM_ERR_INVALID_ARG;
+    *info = dwm_rms_info_t{plan->rows, plan->C, plan->forward, plan->backward, plan->splits};
+    return DWM_OK;
+}
+
+dwm_status_t dwm_rms_set_stride(dwm_rms_plan_t* plan, const char* tensor, long long stride)
+{
+    const int which = named(kRmsNames, tensor);
+    if (!plan || which < 0 || stride < plan->C) return DWM_ERR_INVALID_ARG;
+    if (plan->rows > 0 && stride > kMostElements / plan->rows) return DWM_ERR_UNSUPPORTED;
+    plan->stride[which] = stride;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_rms_set_variant(dwm_rms_plan_t* plan, const char* stage, int variant)
+{
+    if (!plan || !stage) return DWM_ERR_INVALID_ARG;
+    const bool backward = !std::strcmp(stage, "backward");
+    if (!backward && std::strcmp(stage, "forward")) return DWM_ERR_INVALID_ARG;
+    if (backward && plan->ws) return DWM_ERR_WORKSPACE;
+    const int v = variant < 0 ? rms_choice(plan->rows, plan->C, backward) : variant;
+    if (!rms_fits(v, plan->C, backward)) return DWM_ERR_INVALID_ARG;
+    (backward ? plan->backward : plan->forward) = v;
+    plan->splits = rms_splits(plan->rows, plan->C, plan->backward);
+    return DWM_OK;
+}
+
+size_t dwm_rms_workspace_bytes(const dwm_rms_plan_t* plan) { return plan ? (size_t)plan->splits * plan->C * sizeof(float) : 0; }
+
+dwm_status_t dwm_rms_set_workspace(dwm_rms_plan_t* plan, void* ws_dev, size_t bytes)
+{
+    if (!plan) return DWM_ERR_INVALID_ARG;
+    if (!ws_dev || !aligned(ws_dev, 256) || bytes < dwm_rms_workspace_bytes(plan)) return DWM_ERR_WORKSPACE;
+    plan->ws = ws_dev;
+    return DWM_OK;
+}
+
+static RmsArgs rms_args(const dwm_rms_plan& p)
+{
+    RmsArgs a{};
+    std::memcpy(a.stride, p.stride, sizeof(a.stride));
+    a.rows = p.rows;
+    a.C = p.C;
+    a.param_typed = p.param_type == p.type && p.type != DWM_F32;
+    a.splits = p.splits;
+    a.eps = p.eps;
+    return a;
+}
+
+dwm_status_t dwm_rms_forward(const dwm_rms_plan_t* plan, const void* x_dev, const void* residual_dev, const void* gamma_dev, void* z_dev,
+                             void* y_dev, const dwm_packed_t* y_packed, const dwm_packed_t* kept, float* rstd_dev, void* stream)
+{
+    if (!plan || (z_dev && !residual_dev) || !packed_ok(y_packed) || !packed_ok(kept)) return DWM_ERR_INVALID_ARG;
+    if (plan->rows > 0 && (!x_dev || !(z_dev || y_dev || y_packed || kept || rstd_dev))) return DWM_ERR_INVALID_ARG;
+    const size_t size = size_of(plan->type);
+    if (!aligned(x_dev, size) || !aligned(residual_dev, size) || !aligned(z_dev, size) || !aligned(y_dev, size) ||
+        !aligned(gamma_dev, size_of(plan->param_type)) || !aligned(rstd_dev, 4))
+        return DWM_ERR_INVALID_ARG;
+    if (plan->rows == 0) return DWM_OK;
+    RmsArgs a = rms_args(*plan);
+    a.x = x_dev;
+    a.residual = residual_dev;
+    a.gamma = gamma_dev;
+    a.z = z_dev;
+    a.y = y_dev;
+    a.packed_y = packed_of(y_packed);
+    a.kept = packed_of(kept);
+    a.rstd = rstd_dev;
+    return launch_rms_forward(a, plan->type, plan->forward, stream);
+}
+
+dwm_status_t dwm_rms_backward(const dwm_rms_plan_t* plan, const void* dy_dev, const void* dz_dev, const void* z_dev, const dwm_packed_t* kept,
+                              const void* gamma_dev, const float* rstd_dev, void* dx_dev, void* dgamma_dev, void* stream)
+{
+    if (!plan || !packed_ok(kept) || (z_dev && kept) || (!dx_dev && !dgamma_dev)) return DWM_ERR_INVALID_ARG;
+    if (plan->rows > 0 && (!dy_dev || !rstd_dev || !(z_dev || kept))) return DWM_ERR_INVALID_ARG;
+    const size_t size = size_of(plan->type), param = size_of(plan->param_type);
+    if (!aligned(dy_dev, size) || !aligned(dz_dev, size) || !aligned(z_dev, size) || !aligned(dx_dev, size) || !aligned(gamma_dev, param) ||
+        !aligned(dgamma_dev, param) || !aligned(rstd_dev, 4))
+        return DWM_ERR_INVALID_ARG;
+    if (dgamma_dev && !plan->ws) return DWM_ERR_WORKSPACE;
+    if (plan->rows == 0) return dgamma_dev ? launch_columns(nullptr, 0, plan->C, dgamma_dev, plan->param_type, stream) : DWM_OK;
+    RmsArgs a = rms_args(*plan);
+    a.dy = dy_dev;
+    a.dz = dz_dev;
+    a.z = const_cast<void*>(z_dev);
+    a.kept = packed_of(kept);
+    a.gamma = gamma_dev;
+    a.rstd = const_cast<float*>(rstd_dev);
+    a.dx = dx_dev;
+    a.partial = dgamma_dev ? (float*)plan->ws : nullptr;
+    const dwm_status_t st = launch_rms_backward(a, plan->type, plan->backward, stream);
+    return st != DWM_OK || !dgamma_dev ? st : launch_columns(a.partial, plan->splits, plan->C, dgamma_dev, plan->param_type, stream);
+}
+
+dwm_status_t dwm_act_plan_create(dwm_act_plan_t** out, dwm_act_t act, long long rows, int C, dwm_type_t type, dwm_type_t param_type)
+{
+    if (!out || !known(act) || rows < 0 || C < 1 || !known(type) || !(param_type == DWM_F32 || param_type == type)) return DWM_ERR_INVALID_ARG;
+    if (!rows_fit(rows, C)) return DWM_ERR_UNSUPPORTED;
+    dwm_act_plan* p = new (std::nothrow) dwm_act_plan;
+    if (!p) return DWM_ERR_ALLOC;
+    std::memset(p, 0, sizeof(*p));
+    p->rows = rows;
+    p->C = C;
+    p->type = type;
+    p->param_type = param_type;
+    p->act = act;
+    for (long long& s : p->stride) s = C;
+    p->splits = act_splits(rows, C);
+    *out = p;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_act_plan_destroy(dwm_act_plan_t* plan)
+{
+    if (!plan) return DWM_ERR_INVALID_ARG;
+    delete plan;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_act_set_stride(dwm_act_plan_t* plan, const char* tensor, long long stride)
+{
+    const int which = named(kActNames, tensor);
+    if (!plan || which < 0 || stride < plan->C) return DWM_ERR_INVALID_ARG;
+    if (plan->rows > 0 && stride > kMostElements / plan->rows) return DWM_ERR_UNSUPPORTED;
+    plan->stride[which] = stride;
+    return DWM_OK;
+}
+
+size_t dwm_act_workspace_bytes(const dwm_act_plan_t* plan) { return plan ? (size_t)plan->splits * plan->C * sizeof(float) : 0; }
+
+dwm_status_t dwm_act_set_workspace(dwm_act_plan_t* plan, void* ws_dev, size_t bytes)
+{
+    if (!plan) return DWM_ERR_INVALID_ARG;
+    if (!ws_dev || !aligned(ws_dev, 256) || bytes < dwm_act_workspace_bytes(plan)) return DWM_ERR_WORKSPACE;
+    plan->ws = ws_dev;
+    return DWM_OK;
+}
+
+static ActArgs act_args(const dwm_act_plan& p)
+{
+    ActArgs a{};
+    std::memcpy(a.stride, p.stride, sizeof(a.stride));
+    a.rows = p.rows;
+    a.C = p.C;
+    a.param_typed = p.param_type == p.type && p.type != DWM_F32;
+    a.splits = p.splits;
+    a.act = p.act;
+    return a;
+}
+
+dwm_status_t dwm_act_forward(const dwm_act_plan_t* plan, const void* x_dev, const void* bias_dev, void* y_dev, const dwm_packed_t* kept, void* stream)
+{
+    if (!plan || !packed_ok(kept) || (plan->rows > 0 && (!x_dev || !(y_dev || kept)))) return DWM_ERR_INVALID_ARG;
+    const size_t size = size_of(plan->type);
+    if (!aligned(x_dev, size) || !aligned(y_dev, size) || !aligned(bias_dev, size_of(plan->param_type))) return DWM_ERR_INVALID_ARG;
+    if (plan->rows == 0) return DWM_OK;
+    ActArgs a = act_args(*plan);
+    a.x = x_dev;
+    a.bias = bias_dev;
+    a.y = y_dev;
+    a.kept = packed_of(kept);
+    return launch_act_forward(a, plan->type, stream);
+}
+
+dwm_status_t dwm_act_backward(const dwm_act_plan_t* plan, const void* dy_dev, const void* x_dev, const void* bias_dev, const dwm_packed_t* kept,
+                              void* dx_dev, void* dbias_dev, void* stream)
+{
+    if (!plan || !packed_ok(kept) || (kept && (x_dev || bias_dev)) || (bias_dev && !x_dev) || (!dx_dev && !dbias_dev)) return DWM_ERR_INVALID_ARG;
+    if (plan->rows > 0 && (!dy_dev || !(x_dev || kept || plan->act == DWM_ACT_NONE))) return DWM_ERR_INVALID_ARG;
+    const size_t size = size_of(plan->type), param = size_of(plan->param_type);
+    if (!aligned(dy_dev, size) || !aligned(x_dev, size) || !aligned(dx_dev, size) || !aligned(bias_dev, param) || !aligned(dbias_dev, param))
+        return DWM_ERR_INVALID_ARG;
+    if (dbias_dev && !plan->ws) return DWM_ERR_WORKSPACE;
+    if (plan->rows == 0) return dbias_dev ? launch_columns(nullptr, 0, plan->C, dbias_dev, plan->param_type, stream) : DWM_OK;
+    ActArgs a = act_args(*plan);
+    a.dy = dy_dev;
+    if (plan->act != DWM_ACT_NONE) {  // (a derivative of one needs no p)
+        a.x = x_dev;
+        a.bias = bias_dev;
+        a.kept = packed_of(kept);
+    }
+    a.dx = dx_dev;
+    a.partial = dbias_dev ? (float*)plan->ws : nullptr;
+    const dwm_status_t st = launch_act_backward(a, plan->type, stream);
+    return st != DWM_OK || !dbias_dev ? st : launch_columns(a.partial, plan->splits, plan->C, dbias_dev, plan->param_type, stream);
+}
+
+dwm_status_t dwm_matmul_plan_create(dwm_matmul_plan_t** out, int M, int N, int K, dwm_type_t operands, dwm_type_t type, dwm_type_t param_type,
+                                    dwm_act_t act, int flags)
+{
+    const int most = 1 << 24;
+    if (!out || M < 0 || N < 0 || K < 0 || !known(act) || (flags & ~(DWM_A_ACROSS | DWM_B_ACROSS)) || !known(type) ||
+        !(known(operands) || operands == DWM_PACKED) || !(param_type == DWM_F32 || param_type == (operands == DWM_PACKED ? type : operands)))
+        return DWM_ERR_INVALID_ARG;
+    if (operands == DWM_F32 || (operands == DWM_PACKED ? type == DWM_F32 || flags : type != DWM_F32 && type != operands)) return DWM_ERR_UNSUPPORTED;
+    if (M > most || N > most || K > most || (long long)M * N > kMostElements >> 3) return DWM_ERR_UNSUPPORTED;
+    dwm_matmul_plan* p = new (std::nothrow) dwm_matmul_plan;
+    if (!p) return DWM_ERR_ALLOC;
+    std::memset(p, 0, sizeof(*p));
+    p->M = M;
+    p->N = N;
+    p->K = K;
+    p->flags = flags;
+    p->operands = operands;
+    p->type = type;
+    p->param_type = param_type;
+    p->act = act;
+    p->stride[kMatA] = flags & DWM_A_ACROSS ? M : K;
+    p->stride[kMatB] = flags & DWM_B_ACROSS ? N : K;
+    p->stride[kMatResidual] = p->stride[kMatOut] = N;
+    matmul_plan(*p, matmul_choice(*p), -1);
+    *out = p;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_matmul_plan_destroy(dwm_matmul_plan_t* plan)
+{
+    if (!plan) return DWM_ERR_INVALID_ARG;
+    delete plan;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_matmul_plan_info(const dwm_matmul_plan_t* plan, dwm_matmul_info_t* info)
+{
+    if (!plan || !info) return DWM_ERR_INVALID_ARG;
+    *info = dwm_matmul_info_t{plan->M, plan->N, plan->K, plan->shape.kernel, plan->shape.splits};
+    return DWM_OK;
+}
+
+dwm_status_t dwm_matmul_set_stride(dwm_matmul_plan_t* plan, const char* tensor, long long stride)
+{
+    const int which = named(kMatNames, tensor);
+    if (!plan || which < 0 || (plan->operands == DWM_PACKED && which <= kMatB)) return DWM_ERR_INVALID_ARG;
+    const bool across = plan->flags & (which == kMatA ? DWM_A_ACROSS : which == kMatB ? DWM_B_ACROSS : 0);
+    const long long own = which == kMatA ? plan->M : which == kMatB ? plan->N : plan->M;  // rows of a tensor whose rows run along K or N
+    const long long rows = across ? plan->K : own, width = across ? own : which <= kMatB ? plan->K : plan->N;
+    if (stride < width) return DWM_ERR_INVALID_ARG;
+    if (rows > 0 && stride > kMostElements / rows) return DWM_ERR_UNSUPPORTED;
+    plan->stride[which] = stride;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, int variant)
+{
+    if (!plan || !stage) return DWM_ERR_INVALID_ARG;
+    const bool kernel = !std::strcmp(stage, "kernel");
+    if (!kernel && std::strcmp(stage, "splits")) return DWM_ERR_INVALID_ARG;
+    if (plan->ws) return DWM_ERR_WORKSPACE;
+    if (kernel) {
+        const int v = variant < 0 ? matmul_choice(*plan) : variant;
+        if (!matmul_applies(*plan, v)) return DWM_ERR_INVALID_ARG;
+        matmul_plan(*plan, v, -1);
+    } else {
+        if (variant == 0 || variant > 64 || (variant > 1 && plan->shape.kernel == kMatFew)) return DWM_ERR_INVALID_ARG;
+        matmul_plan(*plan, plan->shape.kernel, variant);
+    }
+    return DWM_OK;
+}
+
+size_t dwm_matmul_workspace_bytes(const dwm_matmul_plan_t* plan)
+{
+    if (!plan) return 0;
+    const int splits = plan->shape.splits > plan->any.splits ? plan->shape.splits : plan->any.splits;
+    return splits > 1 ? (size_t)splits * plan->M * matmul_partial_width(plan->N) * sizeof(float) : 0;
+}
+
+dwm_status_t dwm_matmul_set_workspace(dwm_matmul_plan_t* plan, void* ws_dev, size_t bytes)
+{
+    if (!plan) return DWM_ERR_INVALID_ARG;
+    if (!ws_dev || !aligned(ws_dev, 256) || bytes < dwm_matmul_workspace_bytes(plan)) return DWM_ERR_WORKSPACE;
+    plan->ws = ws_dev;
+    return DWM_OK;
+}
+
+dwm_status_t dwm_matmul(const dwm_matmul_plan_t* plan, const void* a_dev, const void* b_dev, const void* bias_dev, const void* residual_dev,
+                        void* out_dev, const dwm_packed_t* y_packed, const dwm_packed_t* kept, void* stream)
+{
+    if (!plan || plan->operands == DWM_PACKED || !matmul_ok(*plan, bias_dev, residual_dev, out_dev, y_packed, kept)) return DWM_ERR_INVALID_ARG;
+    const bool some = plan->M > 0 && plan->N > 0;
+    if ((some && plan->K > 0 && (!a_dev || !b_dev)) || !aligned(a_dev, 2) || !aligned(b_dev, 2)) return DWM_ERR_INVALID_ARG;
+    if (!some) return DWM_OK;
+    MatmulArgs a{};
+    a.a = a_dev;
+    a.b = b_dev;
+    const bool fast = operand_aligned(a_dev, plan->stride[kMatA], plan->flags & DWM_A_ACROSS ? plan->M : plan->K) &&
+                      operand_aligned(b_dev, plan->stride[kMatB], plan->flags & DWM_B_ACROSS ? plan->N : plan->K);
+    return run_matmul(*plan, a, fast ? plan->shape : plan->any, bias_dev, residual_dev, out_dev, y_packed, kept, stream);
+}
+
+dwm_status_t dwm_matmul_packed(const dwm_matmul_plan_t* plan, const dwm_packed_t* a, const dwm_packed_t* b, const void* bias_dev,
+                               const void* residual_dev, void* out_dev, const dwm_packed_t* y_packed, const dwm_packed_t* kept, void* stream)
+{
+    if (!plan || plan->operands != DWM_PACKED || !matmul_ok(*plan, bias_dev, residual_dev, out_dev, y_packed, kept) || !packed_ok(a) || !packed_ok(b))
+        return DWM_ERR_INVALID_ARG;
+    const bool some = plan->M > 0 && plan->N > 0;
+    if (some && plan->K > 0 && (!a || !b)) return DWM_ERR_INVALID_ARG;
+    if (!some) return DWM_OK;
+    MatmulArgs args{};
+    if (a && b) {
+        args.a = a->codes;
+        args.a_scales = (const uint8_t*)a->scales;
+        args.b = b->codes;
+        args.b_scales = (const uint8_t*)b->scales;
+    }
+    return run_matmul(*plan, args, plan->shape, bias_dev, residual_dev, out_dev, y_packed, kept, stream);
+}
+
+}  // extern "C"

@@ -28,6 +28,15 @@ __device__ __forceinline__ void dma16s(const float* base_uniform, uint32_t lane_
                  : "memory");
 }
 
+// Four bytes a lane: lane i's at g land at lds_byte_addr_uniform + 4 * i.
+__device__ __forceinline__ void dma4(const void* g, uint32_t lds_byte_addr_uniform)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+                 :
+                 : "v"(g), "s"(lds_byte_addr_uniform)
+                 : "memory");
+}
+
 template <int N>
 __device__ __forceinline__ void wait_vmcnt()
 {

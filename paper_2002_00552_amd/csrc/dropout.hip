@@ -51,8 +51,8 @@ dwm_status_t launch_dropout(const DropArgs& d, dwm_type_t type, long long n, con
         case DWM_F32: return launch<float>(d, n, x, y, s);
         case DWM_F16: return launch<_Float16>(d, n, x, y, s);
         case DWM_BF16: return launch<__bf16>(d, n, x, y, s);
+        default: return DWM_ERR_INVALID_ARG;
     }
-    return DWM_ERR_INVALID_ARG;
 }
 
 }  // namespace dwm

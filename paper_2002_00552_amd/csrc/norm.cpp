@@ -181,8 +181,8 @@ static dwm_status_t run_kernel(const dwm_norm_plan& p, const NormArgs& a, const 
         case DWM_F32: return launch_norm_f32(a, shape, backward, join, stream);
         case DWM_F16: return launch_norm_f16(a, shape, backward, join, stream);
         case DWM_BF16: return launch_norm_bf16(a, shape, backward, join, stream);
+        default: return DWM_ERR_INVALID_ARG;
     }
-    return DWM_ERR_INVALID_ARG;
 }
 
 static dwm_status_t run_forward(const dwm_norm_plan& p, const NormArgs& a, bool join, void* stream)

@@ -285,8 +285,8 @@ dwm_status_t launch_norm_any_forward(const NormArgs& a, dwm_type_t type, bool jo
         case DWM_F32: return forward<float>(a, join, s);
         case DWM_F16: return forward<_Float16>(a, join, s);
         case DWM_BF16: return forward<__bf16>(a, join, s);
+        default: return DWM_ERR_INVALID_ARG;
     }
-    return DWM_ERR_INVALID_ARG;
 }
 
 dwm_status_t launch_norm_any_backward(const NormArgs& a, dwm_type_t type, void* stream)
@@ -295,8 +295,8 @@ dwm_status_t launch_norm_any_backward(const NormArgs& a, dwm_type_t type, void* 
         case DWM_F32: return backward<float>(a, (hipStream_t)stream);
         case DWM_F16: return backward<_Float16>(a, (hipStream_t)stream);
         case DWM_BF16: return backward<__bf16>(a, (hipStream_t)stream);
+        default: return DWM_ERR_INVALID_ARG;
     }
-    return DWM_ERR_INVALID_ARG;
 }
 
 dwm_status_t launch_norm_params_final(const NormArgs& a, dwm_type_t type, void* stream)
@@ -305,8 +305,8 @@ dwm_status_t launch_norm_params_final(const NormArgs& a, dwm_type_t type, void* 
         case DWM_F32: return params_final<float>(a, (hipStream_t)stream);
         case DWM_F16: return params_final<_Float16>(a, (hipStream_t)stream);
         case DWM_BF16: return params_final<__bf16>(a, (hipStream_t)stream);
+        default: return DWM_ERR_INVALID_ARG;
     }
-    return DWM_ERR_INVALID_ARG;
 }
 
 }  // namespace dwm

@@ -1,0 +1,352 @@
+// Root-mean-square norms of rows with the addition of a residual (gfx950).  Memory bounds them: a row is read once and held in registers, an
+// octet of neighbouring channels to a thread (and one to three more, a row's threads further on), so that four lanes hold a block of
+// 32 channels and its scale comes out of two exchanges between neighbours.  A row's threads are a part of a wave, a wave or a
+// workgroup; the kernels for any size read a row twice.
+#include "norm_device.hpp"
+#include "rows8.hpp"
+
+namespace dwm {
+
+constexpr int rms_threads(int tpr) { return tpr > 256 ? tpr : 256; }
+
+// The sum over a row's threads, for all of them; `slots` has two times sixteen places, used in turn.
+template <int TPR> __device__ __forceinline__ float row_sum(float v, float* slots, int turn)
+{
+    v = lanes_sum<(TPR < 64 ? TPR : 64)>(v);
+    if constexpr (TPR > 64) {
+        constexpr int W = TPR / 64;
+        const int wave = threadIdx.x / 64, first = wave / W * W;
+        float* s = slots + 16 * (turn & 1);
+        s[wave] = v;
+        __syncthreads();
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) v += s[first + i];
+    }
+    return v;
+}
+
+// z of an octet as it is stored: the sum rounded to binary32, then to T; zeros behind the last channel.
+template <class T> __device__ __forceinline__ void joined(float (&z)[8], const float (&r)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) z[j] = (float)(T)(z[j] + r[j]);
+}
+
+// What a row's octet leaves behind: z, y and both in 8 bits.
+template <class T>
+__device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int octet, const float (&z)[8], const float (&gamma)[8], float rstd)
+{
+    const int c = octet * 8, n = a.C - c;
+    if (a.z && n > 0) store_octet<T>((T*)a.z + row * a.stride[kRmsZ] + c, n, z);
+    if (a.kept.codes) {
+        uint32_t s;
+        const uint2v codes = pack_octet<QuadLanes>(z, &s);
+        store_packed(a.kept, row, octet, a.C, codes, s);
+    }
+    if (!a.y && !a.packed_y.codes) return;
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = z[j] * rstd * gamma[j];
+    if (a.y && n > 0) store_octet<T>((T*)a.y + row * a.stride[kRmsY] + c, n, y);
+    if (a.packed_y.codes) {
+        if (n < 8)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = j < n ? y[j] : 0.0f;  // (an infinite rstd makes NaN of zeros)
+        uint32_t s;
+        const uint2v codes = pack_octet<QuadLanes>(y, &s);
+        store_packed(a.packed_y, row, octet, a.C, codes, s);
+    }
+}
+
+template <class T, int TPR, int K> __global__ __launch_bounds__(rms_threads(TPR)) void rms_forward_kernel(RmsArgs a)
+{
+    constexpr int R = rms_threads(TPR) / TPR;
+    __shared__ float slots[32];
+    const int lane = threadIdx.x % TPR;
+    float gamma[K][8];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = (lane + k * TPR) * 8;
+        param_octet<T>(a.gamma, a.param_typed, c, a.C - c, 1.0f, gamma[k]);
+    }
+    int turn = 0;
+    for (long long first = (long long)blockIdx.x * R; first < a.rows; first += (long long)gridDim.x * R, ++turn) {
+        const long long row = first + threadIdx.x / TPR;
+        const bool here = row < a.rows;
+        float z[K][8], r[K][8];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (lane + k * TPR) * 8, n = here ? a.C - c : 0;
+            load_octet<T>((const T*)a.x + (here ? row : 0) * a.stride[kRmsX] + c, n, z[k]);
+            if (a.residual) load_octet<T>((const T*)a.residual + (here ? row : 0) * a.stride[kRmsResidual] + c, n, r[k]);
+        }
+        if (a.residual)
+#pragma unroll
+            for (int k = 0; k < K; ++k) joined<T>(z[k], r[k]);
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum = fmaf(z[k][j], z[k][j], sum);
+        sum = row_sum<TPR>(sum, slots, turn);
+        const float rstd = 1.0f / sqrtf(sum / (float)a.C + a.eps);
+        if (!here) continue;  // (a whole group of lanes; no barrier of this row is left)
+        if (a.rstd && lane == 0) a.rstd[row] = rstd;
+#pragma unroll
+        for (int k = 0; k < K; ++k) rms_write<T>(a, row, lane + k * TPR, z[k], gamma[k], rstd);
+    }
+}
+
+// Any number of channels: a workgroup for a row, read twice.
+template <class T> __global__ __launch_bounds__(1024) void rms_forward_any_kernel(RmsArgs a)
+{
+    __shared__ float slots[32];
+    const int octets = (int)((a.C + kBlock - 1) / kBlock) * 4;
+    int turn = 0;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, ++turn) {
+        float sum = 0.0f;
+        for (int pass = 0; pass < 2; ++pass) {
+            float rstd = 0.0f;
+            if (pass) {
+                sum = row_sum<1024>(sum, slots, turn);
+                rstd = 1.0f / sqrtf(sum / (float)a.C + a.eps);
+                if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+            }
+            for (int octet = threadIdx.x; octet < octets; octet += 1024) {
+                const int c = octet * 8, n = a.C - c;
+                float z[8], r[8], gamma[8];
+                load_octet<T>((const T*)a.x + row * a.stride[kRmsX] + c, n, z);
+                if (a.residual) {
+                    load_octet<T>((const T*)a.residual + row * a.stride[kRmsResidual] + c, n, r);
+                    joined<T>(z, r);
+                }
+                if (pass) {
+                    param_octet<T>(a.gamma, a.param_typed, c, n, 1.0f, gamma);
+                    rms_write<T>(a, row, octet, z, gamma, rstd);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum = fmaf(z[j], z[j], sum);
+                }
+            }
+        }
+    }
+}
+
+// An octet of z for the gradient: as it was stored, or what its checkpoint stands for.
+template <class T> __device__ __forceinline__ void kept_octet(const RmsArgs& a, long long row, int octet, int n, float (&z)[8])
+{
+    if (a.kept.codes) {
+        if (n > 0) {
+            uint2v codes;
+            uint32_t s;
+            load_packed(a.kept, row, octet, a.C, &codes, &s);
+            unpack_octet(codes, s, z);
+            if (n < 8)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) z[j] = j < n ? z[j] : 0.0f;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = 0.0f;
+        }
+    } else {
+        load_octet<T>((const T*)a.z + row * a.stride[kRmsZ] + octet * 8, n, z);
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void rms_gradient(const RmsArgs& a, long long row, int c, int n, const float (&dy)[8], const float (&z)[8], const float (&gamma)[8],
+                                             float rstd, float along)
+{
+    if (n <= 0) return;
+    float dz[8] = {0, 0, 0, 0, 0, 0, 0, 0}, dx[8];
+    if (a.dz) load_octet<T>((const T*)a.dz + row * a.stride[kRmsDz] + c, n, dz);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dx[j] = dz[j] + rstd * (dy[j] * gamma[j] - z[j] * rstd * along);
+    store_octet<T>((T*)a.dx + row * a.stride[kRmsDx] + c, n, dx);
+}
+
+// The gradient, and a workgroup's sums of dy * xhat over its rows for dgamma: in registers, over its groups of lanes through LDS.
+template <class T, int TPR, int K> __global__ __launch_bounds__(rms_threads(TPR)) void rms_backward_kernel(RmsArgs a)
+{
+    constexpr int R = rms_threads(TPR) / TPR;
+    __shared__ float slots[32];
+    __shared__ float sums[R > 1 ? R * TPR * K * 8 : 1];
+    const int lane = threadIdx.x % TPR;
+    float gamma[K][8], acc[K][8];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = (lane + k * TPR) * 8;
+        param_octet<T>(a.gamma, a.param_typed, c, a.C - c, 1.0f, gamma[k]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[k][j] = 0.0f;
+    }
+    int turn = 0;
+    for (long long first = (long long)blockIdx.x * R; first < a.rows; first += (long long)gridDim.x * R, ++turn) {
+        const bool here = first + threadIdx.x / TPR < a.rows;
+        const long long row = here ? first + threadIdx.x / TPR : 0;
+        float dy[K][8], z[K][8];
+        const float rstd = here ? a.rstd[row] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int octet = lane + k * TPR, n = here ? a.C - octet * 8 : 0;
+            load_octet<T>((const T*)a.dy + row * a.stride[kRmsDy] + octet * 8, n, dy[k]);
+            kept_octet<T>(a, row, octet, n, z[k]);
+        }
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float xhat = z[k][j] * rstd;
+                if (here) acc[k][j] = fmaf(dy[k][j], xhat, acc[k][j]);
+                sum = fmaf(dy[k][j] * gamma[k][j], xhat, sum);
+            }
+        if (!a.dx) continue;
+        const float along = row_sum<TPR>(sum, slots, turn) / (float)a.C;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (lane + k * TPR) * 8;
+            rms_gradient<T>(a, row, c, here ? a.C - c : 0, dy[k], z[k], gamma[k], rstd, along);
+        }
+    }
+    if (!a.partial) return;
+    float* to = a.partial + (long long)blockIdx.x * a.C;
+    if constexpr (R == 1) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (lane + k * TPR) * 8;
+            if (c < a.C) store_octet<float>(to + c, a.C - c, acc[k]);
+        }
+    } else {
+        constexpr int W = TPR * K * 8;
+        const int group = threadIdx.x / TPR;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sums[group * W + (lane + k * TPR) * 8 + j] = acc[k][j];
+        __syncthreads();
+        for (int c = threadIdx.x; c < W && c < a.C; c += rms_threads(TPR)) {
+            float s = 0.0f;
+#pragma unroll
+            for (int g = 0; g < R; ++g) s += sums[g * W + c];
+            to[c] = s;
+        }
+    }
+}
+
+// Any number of channels, dx: a workgroup for a row, read twice.  dgamma has a kernel of its own, before dx may overwrite dy.
+template <class T> __global__ __launch_bounds__(1024) void rms_backward_any_kernel(RmsArgs a)
+{
+    __shared__ float slots[32];
+    const int octets = (a.C + 7) / 8;
+    int turn = 0;
+    for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, ++turn) {
+        const float rstd = a.rstd[row];
+        float sum = 0.0f, along = 0.0f;
+        for (int pass = 0; pass < 2; ++pass) {
+            if (pass) along = row_sum<1024>(sum, slots, turn) / (float)a.C;
+            for (int octet = threadIdx.x; octet < octets; octet += 1024) {
+                const int c = octet * 8, n = a.C - c;
+                float dy[8], z[8], gamma[8];
+                load_octet<T>((const T*)a.dy + row * a.stride[kRmsDy] + c, n, dy);
+                kept_octet<T>(a, row, octet, n, z);
+                param_octet<T>(a.gamma, a.param_typed, c, n, 1.0f, gamma);
+                if (pass) {
+                    rms_gradient<T>(a, row, c, n, dy, z, gamma, rstd, along);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum = fmaf(dy[j] * gamma[j], z[j] * rstd, sum);
+                }
+            }
+        }
+    }
+}
+
+// A part of the rows for 2048 channels.
+template <class T> __global__ __launch_bounds__(256) void rms_gamma_any_kernel(RmsArgs a)
+{
+    const int octet = blockIdx.x * 256 + threadIdx.x, c = octet * 8, n = a.C - c;
+    if (n <= 0) return;
+    float acc[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (long long row = blockIdx.y; row < a.rows; row += gridDim.y) {
+        const float rstd = a.rstd[row];
+        float dy[8], z[8];
+        load_octet<T>((const T*)a.dy + row * a.stride[kRmsDy] + c, n, dy);
+        kept_octet<T>(a, row, octet, n, z);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = fmaf(dy[j], z[j] * rstd, acc[j]);
+    }
+    store_octet<float>(a.partial + (long long)blockIdx.y * a.C + c, n, acc);
+}
+
+constexpr long long kRmsBlocks = 1 << 20;  // of a launch forward, at most
+
+template <class T, int TPR, int K> static dwm_status_t forward_shape(const RmsArgs& a, hipStream_t s)
+{
+    constexpr int R = rms_threads(TPR) / TPR;
+    const long long blocks = (a.rows + R - 1) / R;
+    hipLaunchKernelGGL((rms_forward_kernel<T, TPR, K>), dim3((unsigned)(blocks < kRmsBlocks ? blocks : kRmsBlocks)), dim3(rms_threads(TPR)), 0, s, a);
+    return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
+}
+template <class T, int TPR, int K> static dwm_status_t backward_shape(const RmsArgs& a, hipStream_t s)
+{
+    hipLaunchKernelGGL((rms_backward_kernel<T, TPR, K>), dim3(a.splits), dim3(rms_threads(TPR)), 0, s, a);
+    return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
+}
+
+template <class T, int I> static dwm_status_t shaped(const RmsArgs& a, int kernel, bool backward, hipStream_t s)
+{
+    if constexpr (I < kRmsShapeCount) {
+        constexpr RmsShape sh = kRmsShapes[I];
+        if (kernel != I + 1) return shaped<T, I + 1>(a, kernel, backward, s);
+        if constexpr (sh.backward)
+            if (backward) return backward_shape<T, sh.tpr, sh.k>(a, s);
+        if constexpr (sh.forward)
+            if (!backward) return forward_shape<T, sh.tpr, sh.k>(a, s);
+    }
+    return DWM_ERR_INVALID_ARG;
+}
+
+template <class T> static dwm_status_t forward(const RmsArgs& a, int kernel, hipStream_t s)
+{
+    if (kernel > 0) return shaped<T, 0>(a, kernel, false, s);
+    hipLaunchKernelGGL(rms_forward_any_kernel<T>, dim3((unsigned)(a.rows < kRmsBlocks ? a.rows : kRmsBlocks)), dim3(1024), 0, s, a);
+    return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
+}
+
+template <class T> static dwm_status_t backward(const RmsArgs& a, int kernel, hipStream_t s)
+{
+    if (kernel > 0) return shaped<T, 0>(a, kernel, true, s);
+    if (a.partial) {
+        hipLaunchKernelGGL(rms_gamma_any_kernel<T>, dim3((a.C + 2047) / 2048, a.splits), dim3(256), 0, s, a);
+        if (hipGetLastError() != hipSuccess) return DWM_ERR_HIP;
+    }
+    if (!a.dx) return DWM_OK;
+    hipLaunchKernelGGL(rms_backward_any_kernel<T>, dim3((unsigned)(a.rows < kRmsBlocks ? a.rows : kRmsBlocks)), dim3(1024), 0, s, a);
+    return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
+}
+
+dwm_status_t launch_rms_forward(const RmsArgs& a, dwm_type_t type, int kernel, void* stream)
+{
+    const hipStream_t s = (hipStream_t)stream;
+    switch (type) {
+        case DWM_F32: return forward<float>(a, kernel, s);
+        case DWM_F16: return forward<_Float16>(a, kernel, s);
+        case DWM_BF16: return forward<__bf16>(a, kernel, s);
+        default: return DWM_ERR_INVALID_ARG;
+    }
+}
+
+dwm_status_t launch_rms_backward(const RmsArgs& a, dwm_type_t type, int kernel, void* stream)
+{
+    const hipStream_t s = (hipStream_t)stream;
+    switch (type) {
+        case DWM_F32: return backward<float>(a, kernel, s);
+        case DWM_F16: return backward<_Float16>(a, kernel, s);
+        case DWM_BF16: return backward<__bf16>(a, kernel, s);
+        default: return DWM_ERR_INVALID_ARG;
+    }
+}
+
+}  // namespace dwm

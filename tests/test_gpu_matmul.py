@@ -1,0 +1,137 @@
+"""Matrix products with their epilogue through the C ABI against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import branch_reference as ref
+import paper_2002_00552_amd as dwm
+from branch_gpu import ACT, TYPE, PackedRows, Plan, Rows, n64, normal, param, ptr, stream, within
+from test_gpu_rms import packed_within
+
+pytestmark = pytest.mark.gpu
+
+
+def check(M, N, K, operands="bf16", dtype=None, params="f32", act="none", flags=0, bias=True, residual=True, packed=False, wide=0, off=0, variants=None, inplace=False, seed=3):
+    dtype = dtype or ("bf16" if operands == "packed" else operands)
+    print("matmul", M, N, K, operands, dtype, params, act, flags, bias, residual, packed, wide, off, variants, flush=True)
+    av, bv = normal(M, K, seed), normal(N, K, seed + 1) / np.sqrt(max(K, 1))
+    if operands == "packed":
+        a, b = PackedRows(M, K, av) if K else None, PackedRows(N, K, bv) if K else None
+        a64, b64 = (t.values() if K else np.zeros((n, 0)) for t, n in ((a, M), (b, N)))
+    else:
+        a = Rows(K, M, operands, wide, off, av.T) if flags & dwm.DWM_A_ACROSS else Rows(M, K, operands, wide, off, av)
+        b = Rows(K, N, operands, wide, off, bv.T) if flags & dwm.DWM_B_ACROSS else Rows(N, K, operands, wide, off, bv)
+        a64, b64 = a.numpy(), b.numpy()
+        a64 = a64.T if flags & dwm.DWM_A_ACROSS else a64
+        b64 = b64.T if flags & dwm.DWM_B_ACROSS else b64
+    bt = param(N, params, seed + 2) if bias else None
+    res = Rows(M, N, dtype, wide, off, normal(M, N, seed + 4)) if residual else None
+    r64 = res.numpy() if residual else 0.0
+    out = res if inplace else Rows(M, N, dtype, wide, off)
+    y8, kept = (PackedRows(M, N), PackedRows(M, N)) if packed else (None, None)
+    strides = {"out": out, "residual": res} if operands == "packed" else {"a": a, "b": b, "out": out, "residual": res}
+    plan = Plan("matmul", M, N, K, TYPE[operands], TYPE[dtype], TYPE[params], ACT[act], flags, strides=strides, variants=variants)
+    try:
+        tail = (ptr(bt), ptr(res), out.ptr(), y8.t if packed else None, kept.t if packed else None, stream())
+        if operands == "packed":
+            dwm.dwm_matmul_packed(plan.plan, a.t if K else None, b.t if K else None, *tail)
+        else:
+            dwm.dwm_matmul(plan.plan, ptr(a), ptr(b), *tail)
+        torch.cuda.synchronize()
+        p = a64 @ b64.T + (n64(bt) if bias else 0.0)
+        e = ref.matmul_error(a64, b64, operands == "packed") + 2 * ref.U * np.abs(p) + (ref.U * np.abs(n64(bt)) if bias else 0.0)
+        v = ref.act(act, p)
+        ev = 1.2 * e + ref.act_error(act, p)  # (no slope is over 1.13)
+        y = v + r64
+        ev = ev + ref.U * np.abs(y)
+        within(out.numpy(), y, ev + ref.stored(y, dtype), "out")
+        if packed:
+            packed_within(kept, p, e, "kept")
+            packed_within(y8, y, ev, "out in 8 bits")
+        assert out.untouched()
+    finally:
+        plan.close()
+    return out
+
+
+LAYOUTS = [0, dwm.DWM_A_ACROSS, dwm.DWM_B_ACROSS, dwm.DWM_A_ACROSS | dwm.DWM_B_ACROSS]
+
+
+@pytest.mark.parametrize("flags", LAYOUTS)
+@pytest.mark.parametrize("kernel", [0, 1, 2])
+def test_whole_tiles(kernel, flags):
+    for K in (64, 128, 512):
+        check(256, 512, K, flags=flags, variants={"kernel": kernel, "splits": 1}, packed=K == 128, act="gelu" if K == 128 else "none")
+
+
+@pytest.mark.parametrize("flags", LAYOUTS)
+@pytest.mark.parametrize("kernel", [0, 1, 2])
+@pytest.mark.parametrize("operands", ["f16", "bf16"])
+def test_aligned_odd_tiles(operands, kernel, flags):
+    for M, N, K in ((8, 8, 8), (72, 136, 200), (264, 40, 72), (328, 520, 328)):
+        check(M, N, K, operands, flags=flags, variants={"kernel": kernel, "splits": 1}, wide=8, packed=True)
+
+
+@pytest.mark.parametrize("flags", LAYOUTS)
+@pytest.mark.parametrize("operands, dtype, params", [("f16", "f16", "f16"), ("f16", "f32", "f16"), ("bf16", "bf16", "bf16"), ("bf16", "f32", "f32")])
+def test_any_size(operands, dtype, params, flags):
+    for M, N, K in ((1, 1, 1), (3, 5, 7), (65, 33, 129), (130, 257, 77), (200, 100, 1021)):
+        check(M, N, K, operands, dtype, params, act="silu", flags=flags, wide=3, off=1, packed=True)
+
+
+@pytest.mark.parametrize("kernel", [1, 2])
+@pytest.mark.parametrize("dtype, params", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
+def test_packed_operands(dtype, params, kernel):
+    for M, N, K in ((1, 1, 1), (5, 40, 33), (100, 70, 160), (256, 256, 128), (300, 500, 1021)):
+        check(M, N, K, "packed", dtype, params, act="gelu", variants={"kernel": kernel, "splits": 1}, wide=1, packed=True)
+
+
+@pytest.mark.parametrize("operands, kernel", [(o, k) for o in ("f16", "bf16", "packed") for k in range(3) if o != "packed" or k])
+def test_parts_of_k(operands, kernel):
+    for splits in (2, 5, 64):
+        check(136, 264, 1000, operands, act="relu", variants={"kernel": kernel, "splits": splits}, packed=True)
+    check(40, 24, 5000, operands)  # as planned
+
+
+@pytest.mark.parametrize("act", ref.ACTS)
+def test_activations(act):
+    for operands in ("f16", "packed"):
+        check(70, 200, 300, operands, act=act, packed=True)
+        check(70, 200, 304, operands, act=act, bias=False, residual=False)
+
+
+@pytest.mark.parametrize("operands", ["bf16", "packed"])
+def test_no_terms_and_no_elements(operands):
+    check(20, 40, 0, operands, act="silu", packed=True)
+    for M, N in ((0, 8), (8, 0)):
+        plan = Plan("matmul", M, N, 16, TYPE[operands], dwm.DWM_BF16, dwm.DWM_F32, 0, 0)
+        (dwm.dwm_matmul_packed if operands == "packed" else dwm.dwm_matmul)(plan.plan, None, None, None, None, None, None, None, stream())
+        plan.close()
+
+
+def test_sums_in_place():
+    check(100, 200, 300, "bf16", "f32", flags=3, bias=False, inplace=True)
+    check(100, 200, 3000, "f16", flags=1, bias=False, inplace=True, variants={"splits": 4})
+
+
+def test_no_value_of_another_row_gets_in():
+    """NaN in the rows and terms around the operands, and in one row of a: it spoils that row alone."""
+    M, N, K = 70, 90, 100
+    for operands in ("f16", "bf16"):
+        for flags in LAYOUTS:
+            for wide in (0, 4, 11):
+                av, bv = normal(M, K, 1), normal(N, K, 2)
+                a = Rows(*((K, M) if flags & 1 else (M, K)), operands, wide, 0)
+                b = Rows(*((K, N) if flags & 2 else (N, K)), operands, wide, 0)
+                a.buffer.fill_(float("nan"))
+                b.buffer.fill_(float("nan"))
+                av[5, 3] = np.nan
+                a.view.copy_(torch.from_numpy(av.T if flags & 1 else av))
+                b.view.copy_(torch.from_numpy(bv.T if flags & 2 else bv))
+                out = Rows(M, N, operands)
+                plan = Plan("matmul", M, N, K, TYPE[operands], TYPE[operands], dwm.DWM_F32, 0, flags, strides={"a": a, "b": b})
+                dwm.dwm_matmul(plan.plan, a.ptr(), b.ptr(), None, None, out.ptr(), None, None, stream())
+                torch.cuda.synchronize()
+                bad = np.isnan(out.numpy())
+                assert bad[5].all() and not np.delete(bad, 5, axis=0).any()
+                plan.close()
