@@ -89,20 +89,29 @@ template <class T> __global__ __launch_bounds__(256) void act_backward_kernel(Ac
     store_octet<float>(a.partial + (long long)blockIdx.y * a.C + c, n, acc);
 }
 
-// Sixteen channels of a workgroup, sixteen threads along the splits for each, whose sums are then added in their order.
-template <class P> __global__ __launch_bounds__(256) void columns_kernel(const float* partial, int splits, int C, P* out)
+// Sixteen channels of a workgroup and 64 threads along the splits for each: all of a thread's loads go out together, as long as it has
+// no more than sixteen.  The order of the sums is the same in every run.
+template <class P> __global__ __launch_bounds__(1024) void columns_kernel(const float* partial, int splits, int C, P* out)
 {
-    __shared__ float sums[16][17];
-    const int c = blockIdx.x * 16 + threadIdx.x % 16, part = threadIdx.x / 16;
+    __shared__ float sums[64][17];
+    const int lane = threadIdx.x % 16, part = threadIdx.x / 16, c = blockIdx.x * 16 + lane;
     float v = 0.0f;
     if (c < C)
-        for (int s = part; s < splits; s += 16) v += partial[(long long)s * C + c];
-    sums[part][threadIdx.x % 16] = v;
+#pragma unroll 16
+        for (int s = part; s < splits; s += 64) v += partial[(long long)s * C + c];
+    sums[part][lane] = v;
+    __syncthreads();
+    if (part < 16) {
+        v = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v += sums[part + 16 * i][lane];
+        sums[part][lane] = v;  // (read by this thread alone before)
+    }
     __syncthreads();
     if (part || c >= C) return;
     v = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v += sums[i][threadIdx.x];
+    for (int i = 0; i < 16; ++i) v += sums[i][lane];
     out[c] = (P)v;
 }
 
@@ -146,7 +155,7 @@ dwm_status_t launch_act_backward(const ActArgs& a, dwm_type_t type, void* stream
 dwm_status_t launch_columns(const float* partial, int splits, int C, void* out, dwm_type_t type, void* stream)
 {
     const hipStream_t s = (hipStream_t)stream;
-    const dim3 grid((C + 15) / 16), block(256);
+    const dim3 grid((C + 15) / 16), block(1024);
     switch (type) {
         case DWM_F32: hipLaunchKernelGGL(columns_kernel<float>, grid, block, 0, s, partial, splits, C, (float*)out); break;
         case DWM_F16: hipLaunchKernelGGL(columns_kernel<_Float16>, grid, block, 0, s, partial, splits, C, (_Float16*)out); break;

@@ -32,12 +32,13 @@ bool rms_fits(int variant, int C, bool backward)
     return s.tpr * s.k * kOctet >= C && (backward ? s.backward : s.forward);
 }
 
-// The narrowest shape that holds a row: one octet a thread where rows are few, two from 2048 on.
-int rms_choice(long long rows, int C, bool backward)
+// The narrowest shape that holds a row with one octet a thread, or, past 8192 channels, two (16384 rows of 4096 bfloat16, z and y: 256 threads with two octets 116 us,
+// 512 with one 109; backward 114 and 108).
+int rms_choice(int C, bool backward)
 {
-    for (int pass = rows < 2048 ? 0 : 1; pass < 2; ++pass)
+    for (int octets = 1; octets <= 2; ++octets)
         for (int v = 1; v <= kRmsShapeCount; ++v)
-            if (rms_fits(v, C, backward) && (pass == 1 || kRmsShapes[v - 1].k == 1)) return v;
+            if (rms_fits(v, C, backward) && kRmsShapes[v - 1].k == octets) return v;
     return 0;
 }
 
@@ -67,7 +68,7 @@ int matmul_splits(const dwm_matmul_plan& p, int kernel)
     const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step;
     const long long side = kernel == kMat256 ? 256 : 128;
     const long long tiles = ((p.M + side - 1) / side) * ((p.N + side - 1) / side), fill = kernel == kMat256 ? 256 : 512;
-    if (tiles == 0 || kernel == kMatFew) return 1;
+    if (tiles == 0 || kernel >= kMatFew) return 1;
     long long splits = fill / tiles;
     if (splits > steps / 4) splits = steps / 4;
     if (splits > 16) splits = 16;
@@ -76,17 +77,23 @@ int matmul_splits(const dwm_matmul_plan& p, int kernel)
 
 bool matmul_applies(const dwm_matmul_plan& p, int kernel)
 {
-    if (kernel == kMatFew) return false;
+    if (kernel == kMatFew) return p.M <= kMatFewRows && p.flags == 0;
     return kernel == kMatAny ? p.operands != DWM_PACKED : kernel == kMat128 || kernel == kMat256;
 }
 
-int matmul_choice(const dwm_matmul_plan& p) { return p.operands == DWM_PACKED ? kMat128 : kMatAny; }
+int matmul_choice(const dwm_matmul_plan& p)
+{
+    if (matmul_applies(p, kMatFew)) return kMatFew;
+    const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 255) / 256);
+    return tiles >= 128 ? kMat256 : kMat128;
+}
 
 void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
 {
     p.shape.kernel = kernel;
+    if (kernel == kMatFew) splits = 1;
     p.shape.splits = splits > 0 ? splits : matmul_splits(p, kernel);
-    p.any.kernel = p.operands == DWM_PACKED || kernel == kMatFew ? kernel : kMatAny;
+    p.any.kernel = p.operands == DWM_PACKED ? kernel : kernel == kMatFew ? kMatFewLoose : kMatAny;
     p.any.splits = splits > 0 ? splits : matmul_splits(p, p.any.kernel);
 }
 
@@ -195,8 +202,8 @@ dwm_status_t dwm_rms_plan_create(dwm_rms_plan_t** out, long long rows, int C, dw
     p->param_type = param_type;
     p->eps = (float)eps;
     for (long long& s : p->stride) s = C;
-    p->forward = rms_choice(rows, C, false);
-    p->backward = rms_choice(rows, C, true);
+    p->forward = rms_choice(C, false);
+    p->backward = rms_choice(C, true);
     p->splits = rms_splits(rows, C, p->backward);
     *out = p;
     return DWM_OK;
@@ -231,7 +238,7 @@ dwm_status_t dwm_rms_set_variant(dwm_rms_plan_t* plan, const char* stage, int va
     const bool backward = !std::strcmp(stage, "backward");
     if (!backward && std::strcmp(stage, "forward")) return DWM_ERR_INVALID_ARG;
     if (backward && plan->ws) return DWM_ERR_WORKSPACE;
-    const int v = variant < 0 ? rms_choice(plan->rows, plan->C, backward) : variant;
+    const int v = variant < 0 ? rms_choice(plan->C, backward) : variant;
     if (!rms_fits(v, plan->C, backward)) return DWM_ERR_INVALID_ARG;
     (backward ? plan->backward : plan->forward) = v;
     plan->splits = rms_splits(plan->rows, plan->C, plan->backward);

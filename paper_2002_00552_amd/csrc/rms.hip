@@ -9,17 +9,43 @@ namespace dwm {
 
 constexpr int rms_threads(int tpr) { return tpr > 256 ? tpr : 256; }
 
+// The sum over N consecutive lanes in 64 bits, for all of them.
+template <int CTRL> __device__ __forceinline__ double dpp64(double v)
+{
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xf, 0xf, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+template <int N> __device__ __forceinline__ double lanes_sum(double v)
+{
+    v += dpp64<0xB1>(v);
+    if (N >= 4) v += dpp64<0x4E>(v);
+    if (N >= 8) v += dpp64<0x141>(v);
+    if (N >= 16) v += dpp64<0x140>(v);
+#pragma unroll
+    for (int step = 16; step < 64; step *= 2)
+        if (N > step) {
+            const uint64_t u = __builtin_bit_cast(uint64_t, v);
+            const uint32_t lo = (uint32_t)u, hi = (uint32_t)(u >> 32);
+            const auto a = step == 16 ? __builtin_amdgcn_permlane16_swap(lo, lo, false, false) : __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+            const auto b = step == 16 ? __builtin_amdgcn_permlane16_swap(hi, hi, false, false) : __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+            v = __builtin_bit_cast(double, (uint64_t)b[0] << 32 | a[0]) + __builtin_bit_cast(double, (uint64_t)b[1] << 32 | a[1]);
+        }
+    return v;
+}
+
 // The sum over a row's threads, for all of them; `slots` has two times sixteen places, used in turn.
-template <int TPR> __device__ __forceinline__ float row_sum(float v, float* slots, int turn)
+template <int TPR, class F> __device__ __forceinline__ F row_sum(F v, F* slots, int turn)
 {
     v = lanes_sum<(TPR < 64 ? TPR : 64)>(v);
     if constexpr (TPR > 64) {
         constexpr int W = TPR / 64;
         const int wave = threadIdx.x / 64, first = wave / W * W;
-        float* s = slots + 16 * (turn & 1);
+        F* s = slots + 16 * (turn & 1);
         s[wave] = v;
         __syncthreads();
-        v = 0.0f;
+        v = 0;
 #pragma unroll
         for (int i = 0; i < W; ++i) v += s[first + i];
     }
@@ -33,9 +59,25 @@ template <class T> __device__ __forceinline__ void joined(float (&z)[8], const f
     for (int j = 0; j < 8; ++j) z[j] = (float)(T)(z[j] + r[j]);
 }
 
+// rstd from the sum of squares: the hardware's reciprocal root of 64 bits (good to some 26 bits) and a step of Newton's; as two numbers of 32 bits.
+// The squares are summed in 64 bits too, so that y is off by its own rounding and hardly more: what is rounded to 8 bits goes to the other side of a
+// border where a sum in 32 bits has it wrong (a value in some 10^7; memory has time for it).
+struct Rstd {
+    float hi, lo;
+};
+__device__ __forceinline__ Rstd rms_rstd(double sum, const RmsArgs& a)
+{
+    const double m = sum / (double)a.C + (double)a.eps;
+    double r = __builtin_amdgcn_rsq(m);
+    const double better = r * (1.5 - 0.5 * m * r * r);
+    r = better > 0.0 && m > 0.0 ? better : r;  // (zero, infinity and NaN as they are)
+    const float hi = (float)r;
+    return {hi, hi < 3e38f ? (float)(r - (double)hi) : 0.0f};
+}
+
 // What a row's octet leaves behind: z, y and both in 8 bits.
 template <class T>
-__device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int octet, const float (&z)[8], const float (&gamma)[8], float rstd)
+__device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int octet, const float (&z)[8], const float (&gamma)[8], Rstd rstd)
 {
     const int c = octet * 8, n = a.C - c;
     if (a.z && n > 0) store_octet<T>((T*)a.z + row * a.stride[kRmsZ] + c, n, z);
@@ -47,7 +89,10 @@ __device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int o
     if (!a.y && !a.packed_y.codes) return;
     float y[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y[j] = z[j] * rstd * gamma[j];
+    for (int j = 0; j < 8; ++j) {  // one rounding: the product's rest and rstd's go in before it
+        const float t = z[j] * gamma[j], rest = fmaf(z[j], gamma[j], -t);
+        y[j] = fmaf(t, rstd.hi, fmaf(t, rstd.lo, rest * rstd.hi));
+    }
     if (a.y && n > 0) store_octet<T>((T*)a.y + row * a.stride[kRmsY] + c, n, y);
     if (a.packed_y.codes) {
         if (n < 8)
@@ -62,7 +107,7 @@ __device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int o
 template <class T, int TPR, int K> __global__ __launch_bounds__(rms_threads(TPR)) void rms_forward_kernel(RmsArgs a)
 {
     constexpr int R = rms_threads(TPR) / TPR;
-    __shared__ float slots[32];
+    __shared__ double slots[32];
     const int lane = threadIdx.x % TPR;
     float gamma[K][8];
 #pragma unroll
@@ -84,15 +129,14 @@ template <class T, int TPR, int K> __global__ __launch_bounds__(rms_threads(TPR)
         if (a.residual)
 #pragma unroll
             for (int k = 0; k < K; ++k) joined<T>(z[k], r[k]);
-        float sum = 0.0f;
+        double sum = 0.0;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(z[k][j], z[k][j], sum);
-        sum = row_sum<TPR>(sum, slots, turn);
-        const float rstd = 1.0f / sqrtf(sum / (float)a.C + a.eps);
+            for (int j = 0; j < 8; ++j) sum = fma((double)z[k][j], (double)z[k][j], sum);
+        const Rstd rstd = rms_rstd(row_sum<TPR>(sum, slots, turn), a);
         if (!here) continue;  // (a whole group of lanes; no barrier of this row is left)
-        if (a.rstd && lane == 0) a.rstd[row] = rstd;
+        if (a.rstd && lane == 0) a.rstd[row] = rstd.hi;
 #pragma unroll
         for (int k = 0; k < K; ++k) rms_write<T>(a, row, lane + k * TPR, z[k], gamma[k], rstd);
     }
@@ -101,17 +145,16 @@ template <class T, int TPR, int K> __global__ __launch_bounds__(rms_threads(TPR)
 // Any number of channels: a workgroup for a row, read twice.
 template <class T> __global__ __launch_bounds__(1024) void rms_forward_any_kernel(RmsArgs a)
 {
-    __shared__ float slots[32];
+    __shared__ double slots[32];
     const int octets = (int)((a.C + kBlock - 1) / kBlock) * 4;
     int turn = 0;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x, ++turn) {
-        float sum = 0.0f;
+        double sum = 0.0;
         for (int pass = 0; pass < 2; ++pass) {
-            float rstd = 0.0f;
+            Rstd rstd = {0.0f, 0.0f};
             if (pass) {
-                sum = row_sum<1024>(sum, slots, turn);
-                rstd = 1.0f / sqrtf(sum / (float)a.C + a.eps);
-                if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd;
+                rstd = rms_rstd(row_sum<1024>(sum, slots, turn), a);
+                if (a.rstd && threadIdx.x == 0) a.rstd[row] = rstd.hi;
             }
             for (int octet = threadIdx.x; octet < octets; octet += 1024) {
                 const int c = octet * 8, n = a.C - c;
@@ -126,7 +169,7 @@ template <class T> __global__ __launch_bounds__(1024) void rms_forward_any_kerne
                     rms_write<T>(a, row, octet, z, gamma, rstd);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) sum = fmaf(z[j], z[j], sum);
+                    for (int j = 0; j < 8; ++j) sum = fma((double)z[j], (double)z[j], sum);
                 }
             }
         }

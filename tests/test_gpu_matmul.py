@@ -93,6 +93,17 @@ def test_parts_of_k(operands, kernel):
     check(40, 24, 5000, operands)  # as planned
 
 
+@pytest.mark.parametrize("M", [1, 15, 16, 17, 33, 48, 50, 64])
+@pytest.mark.parametrize("operands", ["f16", "bf16", "packed"])
+def test_few_rows(operands, M):
+    for N, K in ((1, 8), (40, 520), (100, 1024), (33, 4000)):
+        check(M, N, K, operands, act="gelu", packed=True, wide=8, variants={"kernel": 3})
+        check(M, N, K, operands, residual=False, variants={"kernel": 3})
+    check(M, 130, 1021, operands, wide=3, off=1)
+    check(M, 64, 0, operands, variants={"kernel": 3})
+    check(M, 16400, 72, operands, variants={"kernel": 3})
+
+
 @pytest.mark.parametrize("act", ref.ACTS)
 def test_activations(act):
     for operands in ("f16", "packed"):
