@@ -672,9 +672,9 @@ DWM_API dwm_status_t dwm_matmul_plan_info(const dwm_matmul_plan_t* plan, dwm_mat
 /* Elements between rows of "a", "b" (16-bit operands), "residual" or "out".  At any time.  16-bit operands whose address is a multiple of 16 and
  * whose stride and row length are multiples of 8 take the faster kernels. */
 DWM_API dwm_status_t dwm_matmul_set_stride(dwm_matmul_plan_t* plan, const char* tensor, long long stride);
-/* For tuning and tests, before dwm_matmul_set_workspace only (DWM_ERR_WORKSPACE afterwards): "kernel": 0 = any alignment (not built for
- * packed operands), 1 = tiles of 128 x 128, 2 = 256 x 256, 3 = few rows (M <= 64, neither operand across); "splits": 1 .. 64; negative: the planner's
- * choice.  DWM_ERR_INVALID_ARG for what does not apply. */
+/* For tuning and tests, before dwm_matmul_set_workspace only (DWM_ERR_WORKSPACE afterwards): "kernel": tiles of 128 x 128 (0) or 64 x 64 (1) of
+ * the result for operands of any alignment, not built for packed ones; 64 x 64 (2), 64 x 128 (3), 128 x 128 (4), 256 x 256 (5) for aligned ones; 6 = few
+ * rows (M <= 64, neither operand across).  "splits": 1 .. 64.  Negative: the planner's choice.  DWM_ERR_INVALID_ARG for what does not apply. */
 DWM_API dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, int variant);
 /* Sums of the parts of K: 256-byte aligned; 0 bytes: not needed. */
 DWM_API size_t dwm_matmul_workspace_bytes(const dwm_matmul_plan_t* plan);

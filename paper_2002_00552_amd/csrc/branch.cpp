@@ -62,12 +62,25 @@ int act_splits(long long rows, int C)
     return (int)(some < 1 ? 1 : some < most ? some : most);
 }
 
-// Tiles of a kernel, the steps of K they go through, and how the parts of K are chosen: as many as fill the 256 CUs, each of some steps.
+struct Tile {
+    int m, n;
+};
+Tile tile_of(int kernel)
+{
+    switch (kernel) {
+        case kMat256: return {256, 256};
+        case kMat64x128: return {64, 128};
+        case kMat64: case kMatAny64: return {64, 64};
+        default: return {128, 128};
+    }
+}
+
+// Parts of K: as many as fill the 256 CUs, each of some steps.
 int matmul_splits(const dwm_matmul_plan& p, int kernel)
 {
     const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step;
-    const long long side = kernel == kMat256 ? 256 : 128;
-    const long long tiles = ((p.M + side - 1) / side) * ((p.N + side - 1) / side), fill = kernel == kMat256 ? 256 : 512;
+    const Tile t = tile_of(kernel);
+    const long long tiles = (long long)((p.M + t.m - 1) / t.m) * ((p.N + t.n - 1) / t.n), fill = kernel == kMat256 ? 256 : 512;
     if (tiles == 0 || kernel >= kMatFew) return 1;
     long long splits = fill / tiles;
     if (splits > steps / 4) splits = steps / 4;
@@ -78,7 +91,7 @@ int matmul_splits(const dwm_matmul_plan& p, int kernel)
 bool matmul_applies(const dwm_matmul_plan& p, int kernel)
 {
     if (kernel == kMatFew) return p.M <= kMatFewRows && p.flags == 0;
-    return kernel == kMatAny ? p.operands != DWM_PACKED : kernel == kMat128 || kernel == kMat256;
+    return kernel <= kMatAny64 ? kernel >= 0 && p.operands != DWM_PACKED : kernel < kMatFew;
 }
 
 int matmul_choice(const dwm_matmul_plan& p)
@@ -90,10 +103,10 @@ int matmul_choice(const dwm_matmul_plan& p)
 
 void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
 {
-    p.shape.kernel = kernel;
     if (kernel == kMatFew) splits = 1;
+    p.shape.kernel = kernel;
     p.shape.splits = splits > 0 ? splits : matmul_splits(p, kernel);
-    p.any.kernel = p.operands == DWM_PACKED ? kernel : kernel == kMatFew ? kMatFewLoose : kMatAny;
+    p.any.kernel = p.operands == DWM_PACKED || kernel <= kMatAny64 ? kernel : kernel == kMatFew ? kMatFewLoose : kernel <= kMat64x128 ? kMatAny64 : kMatAny;
     p.any.splits = splits > 0 ? splits : matmul_splits(p, p.any.kernel);
 }
 

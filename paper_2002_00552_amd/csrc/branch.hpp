@@ -70,7 +70,8 @@ struct MatmulArgs {
     int param_typed, wide_out;  // bias has the operands' 16-bit type, out and residual have 32 bits
     int bf16_out;               // packed operands: the type of out (else binary16)
 };
-enum MatmulKernel { kMatAny, kMat128, kMat256, kMatFew, kMatFewLoose };  // (the last: few rows, of any alignment)
+// Tiles of the result, few rows; the first two and the last (never a plan's own kernel) for operands of any alignment.
+enum MatmulKernel { kMatAny, kMatAny64, kMat64, kMat64x128, kMat128, kMat256, kMatFew, kMatFewLoose };
 constexpr int kMatFewRows = 64;
 struct MatmulShape {
     int kernel, splits;

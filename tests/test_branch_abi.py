@@ -171,7 +171,7 @@ def test_act_calls_that_are_refused(act):
 
 
 def test_matmul_calls_that_are_refused():
-    plan = dwm.dwm_matmul_plan_create(16, 24, 8, F16, F32, F16, 0, 0)
+    plan = dwm.dwm_matmul_plan_create(80, 24, 8, F16, F32, F16, 0, 0)
     packed = dwm.dwm_matmul_plan_create(16, 24, 8, PACKED, BF16, F32, 0, 0)
     ok = P(ONE, ONE)
     try:
@@ -187,13 +187,13 @@ def test_matmul_calls_that_are_refused():
         _refused(BAD, g, plan, ok, ok, None, None, ONE)
         for p, name, stride, status in ((plan, "a", 7, BAD), (plan, "c", 24, BAD), (plan, "out", 23, BAD), (plan, "b", 1 << 40, OUT), (packed, "a", 8, BAD), (packed, "b", 8, BAD)):
             _refused(status, dwm.dwm_matmul_set_stride, p, name, stride)
-        for p, stage, v in ((plan, "kernels", 0), (plan, "kernel", 4), (packed, "kernel", 0), (plan, "splits", 0), (plan, "splits", 65)):
+        for p, stage, v in ((plan, "kernels", 0), (plan, "kernel", 7), (packed, "kernel", 0), (packed, "kernel", 1), (plan, "splits", 0), (plan, "splits", 65)):
             _refused(BAD, dwm.dwm_matmul_set_variant, p, stage, v)
         assert dwm.dwm_matmul_workspace_bytes(plan) == 0
         dwm.dwm_matmul_set_variant(plan, "splits", 3)
-        assert dwm.dwm_matmul_plan_info(plan).splits == 3 and dwm.dwm_matmul_workspace_bytes(plan) == 3 * 16 * 32 * 4
+        assert dwm.dwm_matmul_plan_info(plan).splits == 3 and dwm.dwm_matmul_workspace_bytes(plan) == 3 * 80 * 32 * 4
         _refused(dwm.DWM_ERR_WORKSPACE, f, plan, ONE, ONE, None, None, ONE)
-        for ws, n in ((None, 1 << 20), (ONE + 4, 1 << 20), (ONE, 3 * 16 * 32 * 4 - 1)):
+        for ws, n in ((None, 1 << 20), (ONE + 4, 1 << 20), (ONE, 3 * 80 * 32 * 4 - 1)):
             _refused(dwm.DWM_ERR_WORKSPACE, dwm.dwm_matmul_set_workspace, plan, ws, n)
         dwm.dwm_matmul_set_workspace(plan, ONE, 1 << 20)
         _refused(dwm.DWM_ERR_WORKSPACE, dwm.dwm_matmul_set_variant, plan, "splits", 1)
