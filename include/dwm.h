@@ -673,8 +673,8 @@ DWM_API dwm_status_t dwm_matmul_plan_info(const dwm_matmul_plan_t* plan, dwm_mat
  * whose stride and row length are multiples of 8 take the faster kernels. */
 DWM_API dwm_status_t dwm_matmul_set_stride(dwm_matmul_plan_t* plan, const char* tensor, long long stride);
 /* For tuning and tests, before dwm_matmul_set_workspace only (DWM_ERR_WORKSPACE afterwards): "kernel": tiles of 128 x 128 (0) or 64 x 64 (1) of
- * the result for operands of any alignment, not built for packed ones; 64 x 64 (2), 64 x 128 (3), 128 x 128 (4), 256 x 256 (5) for aligned ones; 6 = few
- * rows (M <= 64, neither operand across).  "splits": 1 .. 64.  Negative: the planner's choice.  DWM_ERR_INVALID_ARG for what does not apply. */
+ * the result for operands of any alignment, not built for packed ones; 64 x 64 (2), 128 x 128 (3), 256 x 256 (4) for aligned ones; 5 = few rows
+ * (M <= 32, neither operand across; never more than one part of K).  "splits": 1 .. 64.  Negative: the planner's choice.  DWM_ERR_INVALID_ARG for what does not apply. */
 DWM_API dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, int variant);
 /* Sums of the parts of K: 256-byte aligned; 0 bytes: not needed. */
 DWM_API size_t dwm_matmul_workspace_bytes(const dwm_matmul_plan_t* plan);

@@ -62,30 +62,35 @@ int act_splits(long long rows, int C)
     return (int)(some < 1 ? 1 : some < most ? some : most);
 }
 
-struct Tile {
-    int m, n;
+// What a tile's kernel takes, in us: a step of K for a workgroup that has a CU to itself, for one of several on every CU (each CU's share), how many
+// a CU holds, and what a workgroup takes before its first and after its last step.  From 50 shapes of 128 to 16384 rows, 64 to 16384 columns and 256
+// to 16384 terms in bfloat16 and 8 bits, each with one to sixteen parts: the choice by these is 3% behind the best on the average and at most a fourth.
+struct MatmulRate {
+    int side;
+    double alone, shared;
+    int held;
+    double ends;
 };
-Tile tile_of(int kernel)
-{
-    switch (kernel) {
-        case kMat256: return {256, 256};
-        case kMat64x128: return {64, 128};
-        case kMat64: case kMatAny64: return {64, 64};
-        default: return {128, 128};
-    }
-}
+const MatmulRate kMatmulRates[] = {
+    {128, 1.8, 1.0, 2, 3.5},   // any alignment
+    {64, 0.8, 0.4, 4, 1.5},    // any alignment
+    {64, 0.42, 0.17, 4, 1.5},  // 512 x 512 x 16384: 111 us, with 128 x 128 tiles 155, in eight parts 25 and 30
+    {128, 0.62, 0.47, 2, 3.5}, // 2048 x 4096 x 1024: 22 us, with 64 x 64 tiles 28, with 256 x 256 29
+    {256, 1.2, 1.5, 1, 8.0},   // 2048 x 8192 x 2048: 58 us, with 128 x 128 tiles 67
+};
 
-// Parts of K: as many as fill the 256 CUs, each of some steps.
-int matmul_splits(const dwm_matmul_plan& p, int kernel)
+double matmul_cost(const dwm_matmul_plan& p, int kernel, int splits)
 {
-    const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step;
-    const Tile t = tile_of(kernel);
-    const long long tiles = (long long)((p.M + t.m - 1) / t.m) * ((p.N + t.n - 1) / t.n), fill = kernel == kMat256 ? 256 : 512;
-    if (tiles == 0 || kernel >= kMatFew) return 1;
-    long long splits = fill / tiles;
-    if (splits > steps / 4) splits = steps / 4;
-    if (splits > 16) splits = 16;
-    return (int)(splits < 1 ? 1 : splits);
+    const double elements = (double)p.N * p.K, launch = 3.5;
+    if (kernel >= kMatFew)  // b once, and a again and again from the L2 (N = 12288, K = 4096 bfloat16, M = 1, 16, 32: 20.8, 26, 36 us, by tiles 20 to 21)
+        return launch + elements * 1e-6 * ((p.operands == DWM_PACKED ? 0.2 : 0.33) + 0.011 * p.M);
+    const MatmulRate& r = kMatmulRates[kernel];
+    const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step, part = (steps + splits - 1) / splits;
+    const double groups = (double)((p.M + r.side - 1) / r.side) * ((p.N + r.side - 1) / r.side) * splits, rounds = groups / (256.0 * r.held);
+    const double each = groups <= 256 ? 1 : rounds >= 1 ? r.held : groups / 256, step_time = each * r.shared > r.alone ? each * r.shared : r.alone;
+    double time = launch + (rounds <= 1 ? 1 : rounds < 4 ? (double)(long long)(rounds + 0.999) : rounds + 0.5) * (part * step_time + r.ends * (each > 2 ? 2 : each > 1 ? 1.4 : 1));
+    if (splits > 1) time += 4 + (double)p.M * p.N * (8.0 * splits + 2) / 6.5e6;  // the parts' sums there and back, and a launch
+    return time;
 }
 
 bool matmul_applies(const dwm_matmul_plan& p, int kernel)
@@ -94,20 +99,37 @@ bool matmul_applies(const dwm_matmul_plan& p, int kernel)
     return kernel <= kMatAny64 ? kernel >= 0 && p.operands != DWM_PACKED : kernel < kMatFew;
 }
 
-int matmul_choice(const dwm_matmul_plan& p)
+// The cheapest of some kernels, with as many parts of K as are asked for or the best number of them, each of four steps at least.
+MatmulShape matmul_shape(const dwm_matmul_plan& p, int first, int last, int splits)
 {
-    if (matmul_applies(p, kMatFew)) return kMatFew;
-    const long long tiles = (long long)((p.M + 255) / 256) * ((p.N + 255) / 256);
-    return tiles >= 128 ? kMat256 : kMat128;
+    MatmulShape best = {first, splits > 0 && first < kMatFew ? splits : 1};
+    double least = -1;
+    const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step;
+    for (int kernel = first; kernel <= last; ++kernel)
+        for (int s = 1; s <= 16; s *= 2) {
+            if (s > 1 && (kernel >= kMatFew || splits > 0 || s * 4 > steps)) continue;
+            const int parts = splits > 0 && kernel < kMatFew ? splits : s;
+            const double cost = matmul_cost(p, kernel, parts);
+            if (least < 0 || cost < least) {
+                least = cost;
+                best = {kernel, parts};
+            }
+        }
+    return best;
 }
 
+// kernel, splits: negative for the planner's choice.
 void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
 {
-    if (kernel == kMatFew) splits = 1;
-    p.shape.kernel = kernel;
-    p.shape.splits = splits > 0 ? splits : matmul_splits(p, kernel);
-    p.any.kernel = p.operands == DWM_PACKED || kernel <= kMatAny64 ? kernel : kernel == kMatFew ? kMatFewLoose : kernel <= kMat64x128 ? kMatAny64 : kMatAny;
-    p.any.splits = splits > 0 ? splits : matmul_splits(p, p.any.kernel);
+    const bool few = matmul_applies(p, kMatFew) && splits <= 1;
+    p.shape = kernel >= 0 ? matmul_shape(p, kernel, kernel, splits) : matmul_shape(p, kMat64, few ? kMatFew : kMat256, splits);
+    if (p.operands == DWM_PACKED || p.shape.kernel <= kMatAny64) {
+        p.any = p.shape;
+    } else if (kernel == kMatFew || (kernel < 0 && few && matmul_cost(p, kMatFewLoose, 1) < matmul_cost(p, kMatAny64, matmul_shape(p, kMatAny64, kMatAny64, splits).splits))) {
+        p.any = {kMatFewLoose, 1};
+    } else {
+        p.any = matmul_shape(p, kMatAny, kMatAny64, splits);
+    }
 }
 
 // Whether the kernels that copy sixteen bytes at a time straight into LDS can read an operand.
@@ -442,7 +464,7 @@ dwm_status_t dwm_matmul_plan_create(dwm_matmul_plan_t** out, int M, int N, int K
     p->stride[kMatA] = flags & DWM_A_ACROSS ? M : K;
     p->stride[kMatB] = flags & DWM_B_ACROSS ? N : K;
     p->stride[kMatResidual] = p->stride[kMatOut] = N;
-    matmul_plan(*p, matmul_choice(*p), -1);
+    matmul_plan(*p, -1, -1);
     *out = p;
     return DWM_OK;
 }
@@ -481,9 +503,8 @@ dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, 
     if (!kernel && std::strcmp(stage, "splits")) return DWM_ERR_INVALID_ARG;
     if (plan->ws) return DWM_ERR_WORKSPACE;
     if (kernel) {
-        const int v = variant < 0 ? matmul_choice(*plan) : variant;
-        if (!matmul_applies(*plan, v)) return DWM_ERR_INVALID_ARG;
-        matmul_plan(*plan, v, -1);
+        if (variant >= 0 && !matmul_applies(*plan, variant)) return DWM_ERR_INVALID_ARG;
+        matmul_plan(*plan, variant < 0 ? -1 : variant, -1);
     } else {
         if (variant == 0 || variant > 64 || (variant > 1 && plan->shape.kernel == kMatFew)) return DWM_ERR_INVALID_ARG;
         matmul_plan(*plan, plan->shape.kernel, variant);

@@ -71,8 +71,8 @@ struct MatmulArgs {
     int bf16_out;               // packed operands: the type of out (else binary16)
 };
 // Tiles of the result, few rows; the first two and the last (never a plan's own kernel) for operands of any alignment.
-enum MatmulKernel { kMatAny, kMatAny64, kMat64, kMat64x128, kMat128, kMat256, kMatFew, kMatFewLoose };
-constexpr int kMatFewRows = 64;
+enum MatmulKernel { kMatAny, kMatAny64, kMat64, kMat128, kMat256, kMatFew, kMatFewLoose };
+constexpr int kMatFewRows = 32;
 struct MatmulShape {
     int kernel, splits;
 };

@@ -187,7 +187,7 @@ def test_matmul_calls_that_are_refused():
         _refused(BAD, g, plan, ok, ok, None, None, ONE)
         for p, name, stride, status in ((plan, "a", 7, BAD), (plan, "c", 24, BAD), (plan, "out", 23, BAD), (plan, "b", 1 << 40, OUT), (packed, "a", 8, BAD), (packed, "b", 8, BAD)):
             _refused(status, dwm.dwm_matmul_set_stride, p, name, stride)
-        for p, stage, v in ((plan, "kernels", 0), (plan, "kernel", 7), (packed, "kernel", 0), (packed, "kernel", 1), (plan, "splits", 0), (plan, "splits", 65)):
+        for p, stage, v in ((plan, "kernels", 0), (plan, "kernel", 6), (plan, "kernel", 5), (packed, "kernel", 0), (packed, "kernel", 1), (plan, "splits", 0), (plan, "splits", 65)):
             _refused(BAD, dwm.dwm_matmul_set_variant, p, stage, v)
         assert dwm.dwm_matmul_workspace_bytes(plan) == 0
         dwm.dwm_matmul_set_variant(plan, "splits", 3)

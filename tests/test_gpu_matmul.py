@@ -58,14 +58,14 @@ LAYOUTS = [0, dwm.DWM_A_ACROSS, dwm.DWM_B_ACROSS, dwm.DWM_A_ACROSS | dwm.DWM_B_A
 
 
 @pytest.mark.parametrize("flags", LAYOUTS)
-@pytest.mark.parametrize("kernel", range(6))
+@pytest.mark.parametrize("kernel", range(5))
 def test_whole_tiles(kernel, flags):
     for K in (64, 128, 512):
         check(256, 512, K, flags=flags, variants={"kernel": kernel, "splits": 1}, packed=K == 128, act="gelu" if K == 128 else "none")
 
 
 @pytest.mark.parametrize("flags", LAYOUTS)
-@pytest.mark.parametrize("kernel", range(6))
+@pytest.mark.parametrize("kernel", range(5))
 @pytest.mark.parametrize("operands", ["f16", "bf16"])
 def test_aligned_odd_tiles(operands, kernel, flags):
     for M, N, K in ((8, 8, 8), (72, 136, 200), (264, 40, 72), (328, 520, 328)):
@@ -79,29 +79,29 @@ def test_any_size(operands, dtype, params, flags):
         check(M, N, K, operands, dtype, params, act="silu", flags=flags, wide=3, off=1, packed=True)
 
 
-@pytest.mark.parametrize("kernel", [2, 3, 4, 5])
+@pytest.mark.parametrize("kernel", [2, 3, 4])
 @pytest.mark.parametrize("dtype, params", [("bf16", "f32"), ("bf16", "bf16"), ("f16", "f16")])
 def test_packed_operands(dtype, params, kernel):
     for M, N, K in ((1, 1, 1), (5, 40, 33), (100, 70, 160), (256, 256, 128), (300, 500, 1021)):
         check(M, N, K, "packed", dtype, params, act="gelu", variants={"kernel": kernel, "splits": 1}, wide=1, packed=True)
 
 
-@pytest.mark.parametrize("operands, kernel", [(o, k) for o in ("f16", "bf16", "packed") for k in range(6) if o != "packed" or k > 1])
+@pytest.mark.parametrize("operands, kernel", [(o, k) for o in ("f16", "bf16", "packed") for k in range(5) if o != "packed" or k > 1])
 def test_parts_of_k(operands, kernel):
     for splits in (2, 5, 64):
         check(136, 264, 1000, operands, act="relu", variants={"kernel": kernel, "splits": splits}, packed=True)
     check(40, 24, 5000, operands)  # as planned
 
 
-@pytest.mark.parametrize("M", [1, 15, 16, 17, 33, 48, 50, 64])
+@pytest.mark.parametrize("M", [1, 2, 15, 16, 17, 31, 32])
 @pytest.mark.parametrize("operands", ["f16", "bf16", "packed"])
 def test_few_rows(operands, M):
     for N, K in ((1, 8), (40, 520), (100, 1024), (33, 4000)):
-        check(M, N, K, operands, act="gelu", packed=True, wide=8, variants={"kernel": 6})
-        check(M, N, K, operands, residual=False, variants={"kernel": 6})
+        check(M, N, K, operands, act="gelu", packed=True, wide=8, variants={"kernel": 5})
+        check(M, N, K, operands, residual=False, variants={"kernel": 5})
     check(M, 130, 1021, operands, wide=3, off=1)
-    check(M, 64, 0, operands, variants={"kernel": 6})
-    check(M, 16400, 72, operands, variants={"kernel": 6})
+    check(M, 64, 0, operands, variants={"kernel": 5})
+    check(M, 16400, 72, operands, variants={"kernel": 5})
 
 
 @pytest.mark.parametrize("act", ref.ACTS)
