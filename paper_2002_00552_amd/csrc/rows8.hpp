@@ -66,44 +66,41 @@ struct QuadLanes {
         return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));
     }
 };
-// ... or half a wave apart (a product's accumulators: two lanes).
-struct HalfApart {
+// ... or sixteen apart (a product's accumulators).
+struct SixteenApart {
     static __device__ __forceinline__ uint32_t most(uint32_t v)
     {
-        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-        return max((uint32_t)r[0], (uint32_t)r[1]);
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        v = max((uint32_t)r[0], (uint32_t)r[1]);
+        const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return max((uint32_t)q[0], (uint32_t)q[1]);
     }
 };
 
 constexpr uint32_t kInfinity = 0x7f800000u;
 
-// The largest magnitude of an octet, as its pattern: as unsigned numbers the patterns of magnitudes are in their order, infinities and NaN last.
-__device__ __forceinline__ uint32_t octet_most(const float (&f)[8])
+// The codes of an octet and its block's scale; all four lanes of the block take part, with zeros behind the last channel.
+// As unsigned numbers the patterns of magnitudes are in their order, infinities and NaN last; only a block that has some looks at each
+// element.  448 is 1.75 * 2^8: the scale is the magnitude's exponent less 8, and one more where its fraction is over 0.75,
+// which the addition carries.  v / 2^(s - 127) is exact but for numbers below the smallest code.
+template <class Lanes> __device__ __forceinline__ uint2v pack_octet(const float (&f)[8], uint32_t* scale)
 {
     uint32_t m = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(f[j]) & 0x7fffffffu);
-    return m;
-}
-__device__ __forceinline__ uint32_t octet_most_finite(const float (&f)[8])
-{
-    uint32_t m = 0;
+    m = Lanes::most(m);
+    if (m >= kInfinity) {  // (all four lanes have the same m)
+        m = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t a = __float_as_uint(f[j]) & 0x7fffffffu;
-        m = max(m, a < kInfinity ? a : 0u);
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t a = __float_as_uint(f[j]) & 0x7fffffffu;
+            m = max(m, a < kInfinity ? a : 0u);
+        }
+        m = Lanes::most(m);
     }
-    return m;
-}
-
-// The scale of a block from its largest finite magnitude: 448 is 1.75 * 2^8, so it is the magnitude's exponent less 8, and one more where its
-// fraction is over 0.75, which the addition carries.
-__device__ __forceinline__ uint32_t scale_of(uint32_t most) { return (uint32_t)max((int)((most + 0x1fffffu) >> 23) - 8, 0); }
-
-// v / 2^(s - 127) is exact but for numbers below the smallest code.
-__device__ __forceinline__ uint2v octet_codes(const float (&f)[8], uint32_t scale)
-{
-    const float by = __uint_as_float((254u - scale) << 23);
+    const int s = max((int)((m + 0x1fffffu) >> 23) - 8, 0);
+    *scale = (uint32_t)s;
+    const float by = __uint_as_float((uint32_t)(254 - s) << 23);
     uint2v codes;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -112,16 +109,6 @@ __device__ __forceinline__ uint2v octet_codes(const float (&f)[8], uint32_t scal
         codes[i] = (uint32_t)w;
     }
     return codes;
-}
-
-// The codes of an octet and its block's scale; all four lanes of the block take part, with zeros behind the last channel.  Only a block that has
-// an infinity or NaN looks at each element again.
-template <class Lanes> __device__ __forceinline__ uint2v pack_octet(const float (&f)[8], uint32_t* scale)
-{
-    uint32_t m = Lanes::most(octet_most(f));
-    if (m >= kInfinity) m = Lanes::most(octet_most_finite(f));  // (all four lanes have the same m)
-    *scale = scale_of(m);
-    return octet_codes(f, *scale);
 }
 
 __device__ __forceinline__ void unpack_octet(uint2v codes, uint32_t scale, float (&f)[8])
