@@ -132,8 +132,11 @@ void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
     }
 }
 
-// Whether the kernels that copy sixteen bytes at a time straight into LDS can read an operand.
-bool operand_aligned(const void* p, long long stride, long long length) { return aligned(p, 16) && stride % 8 == 0 && length % 8 == 0; }
+// Whether the kernels that copy sixteen bytes at a time straight into LDS can read an operand; a tile's 256 rows have to lie within 2^32 bytes.
+bool operand_aligned(const void* p, long long stride, long long length)
+{
+    return aligned(p, 16) && stride % 8 == 0 && length % 8 == 0 && stride <= 1 << 22;
+}
 
 dwm_status_t run_matmul(const dwm_matmul_plan& p, MatmulArgs& a, const MatmulShape& shape, const void* bias, const void* residual,
                         void* out, const dwm_packed_t* packed_y, const dwm_packed_t* kept, void* stream)

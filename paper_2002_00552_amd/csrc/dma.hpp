@@ -37,6 +37,15 @@ __device__ __forceinline__ void dma4(const void* g, uint32_t lds_byte_addr_unifo
                  : "memory");
 }
 
+// The same from a wave-uniform base and the lane's unsigned 32-bit byte offset.
+__device__ __forceinline__ void dma4s(const void* base_uniform, uint32_t lane_byte_offset, uint32_t lds_byte_addr_uniform)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+                 :
+                 : "v"(lane_byte_offset), "s"(base_uniform), "s"(lds_byte_addr_uniform)
+                 : "memory");
+}
+
 template <int N>
 __device__ __forceinline__ void wait_vmcnt()
 {
