@@ -115,13 +115,14 @@ template <class P> __global__ __launch_bounds__(1024) void columns_kernel(const 
     out[c] = (P)v;
 }
 
-constexpr long long kActBlocks = 65535;  // along the rows, at most
+// Workgroups along the rows, at most: fewer than 2^32 threads in all.
+static long long most_blocks(int groups) { return groups > 128 ? (1 << 23) / groups : 65535; }
 
 template <class T> static dwm_status_t forward(const ActArgs& a, hipStream_t s)
 {
-    const int lanes = row_lanes(a.C), rows = 256 / lanes;
-    const long long blocks = (a.rows + rows - 1) / rows;
-    hipLaunchKernelGGL(act_forward_kernel<T>, dim3((a.C + 2047) / 2048, (unsigned)(blocks < kActBlocks ? blocks : kActBlocks)), dim3(256), 0, s, a, shift_of(lanes));
+    const int lanes = row_lanes(a.C), rows = 256 / lanes, groups = (a.C + 2047) / 2048;
+    const long long blocks = (a.rows + rows - 1) / rows, most = most_blocks(groups);
+    hipLaunchKernelGGL(act_forward_kernel<T>, dim3(groups, (unsigned)(blocks < most ? blocks : most)), dim3(256), 0, s, a, shift_of(lanes));
     return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
 }
 template <class T> static dwm_status_t backward(const ActArgs& a, hipStream_t s)

@@ -53,18 +53,21 @@ int rms_splits(long long rows, int C, int kernel)
     return (int)(blocks < 1 ? 1 : blocks < most ? blocks : most);
 }
 
+// Parts of the rows, a workgroup each for 2048 channels: up to 2048 workgroups, of four rows a thread at least where there are that many (16384 rows of 8192 bfloat16, gelu, with
+// the last sums: 1024 workgroups 164 us, 2048 159).
 int act_splits(long long rows, int C)
 {
-    const long long groups = (C + 2047) / 2048, most = groups > 1024 ? 1 : 1024 / groups;
+    const long long groups = (C + 2047) / 2048, most = groups > 2048 ? 1 : 2048 / groups;
     long long lanes = 1;
     while (lanes < 256 && lanes * kOctet < C) lanes *= 2;
-    const long long some = (rows + 4 * (256 / lanes) - 1) / (4 * (256 / lanes));
+    const long long each = (rows + 256 / lanes - 1) / (256 / lanes), per = each * groups >= 2048 ? 4 : each * groups >= 1024 ? 2 : 1, some = (each + per - 1) / per;
     return (int)(some < 1 ? 1 : some < most ? some : most);
 }
 
-// What a tile's kernel takes, in us: a step of K for a workgroup that has a CU to itself, for one of several on every CU (each CU's share), how many
-// a CU holds, and what a workgroup takes before its first and after its last step.  From 50 shapes of 128 to 16384 rows, 64 to 16384 columns and 256
-// to 16384 terms in bfloat16 and 8 bits, each with one to sixteen parts: the choice by these is 3% behind the best on the average and at most a fourth.
+// What a tile's kernel takes, in us: a step of 128 bytes of K for a workgroup that has a CU to itself, for one of several on every CU (each CU's share), how
+// many a CU holds, and what a workgroup takes before its first and after its last step.  From 45 shapes of 1 to 16384 rows, 64 to 16384 columns and 256
+// to 16384 terms in bfloat16 and 8 bits, operands out of the caches, each with one to eight parts: the choice by these is 3% behind the best on the average, a
+// fifth at most.
 struct MatmulRate {
     int side;
     double alone, shared;
@@ -72,24 +75,26 @@ struct MatmulRate {
     double ends;
 };
 const MatmulRate kMatmulRates[] = {
-    {128, 1.8, 1.0, 2, 3.5},   // any alignment
-    {64, 0.8, 0.4, 4, 1.5},    // any alignment
-    {64, 0.42, 0.17, 4, 1.5},  // 512 x 512 x 16384: 111 us, with 128 x 128 tiles 155, in eight parts 25 and 30
-    {128, 0.62, 0.47, 2, 3.5}, // 2048 x 4096 x 1024: 22 us, with 64 x 64 tiles 28, with 256 x 256 29
+    {128, 1.8, 1.0, 2, 3.5},   // any alignment (2000 x 2001 x 2003: 48 us in one part, 44 in two, with 64 x 64 tiles 54)
+    {64, 0.8, 0.4, 4, 1.5},    // any alignment (1000 x 777 x 1021: 16 us, with 128 x 128 tiles 23)
+    {64, 0.32, 0.17, 2, 1.5},  // 512 x 512 x 16384: 93 us, in eight parts 22; 1024 x 1024 x 1024: 8, with 128 x 128 tiles 12
+    {128, 0.68, 0.47, 2, 3.5}, // 2048 x 4096 x 1024: 20 us, with 64 x 64 tiles 31, with 256 x 256 29
     {256, 1.2, 1.5, 1, 8.0},   // 2048 x 8192 x 2048: 58 us, with 128 x 128 tiles 67
 };
 
 double matmul_cost(const dwm_matmul_plan& p, int kernel, int splits)
 {
     const double elements = (double)p.N * p.K, launch = 3.5;
-    if (kernel >= kMatFew)  // b once, and a again and again from the L2 (N = 12288, K = 4096 bfloat16, M = 1, 16, 32: 20.8, 26, 36 us, by tiles 20 to 21)
+    if (kernel >= kMatFew)  // b once, and a again and again from the L2 (N = 12288, K = 4096 bfloat16, M = 1, 16, 32: 22, 32, 43 us, by tiles 24 to 26)
         return launch + elements * 1e-6 * ((p.operands == DWM_PACKED ? 0.2 : 0.33) + 0.011 * p.M);
     const MatmulRate& r = kMatmulRates[kernel];
     const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step, part = (steps + splits - 1) / splits;
+    const bool reads_across = kernel == kMat64 || kernel == kMat128;  // (twice as many LDS reads, and strides of whole rows)
+    const double across = 1 + (reads_across ? 0.15 * (!!(p.flags & DWM_A_ACROSS) + !!(p.flags & DWM_B_ACROSS)) : 0);
     const double groups = (double)((p.M + r.side - 1) / r.side) * ((p.N + r.side - 1) / r.side) * splits, rounds = groups / (256.0 * r.held);
-    const double each = groups <= 256 ? 1 : rounds >= 1 ? r.held : groups / 256, step_time = each * r.shared > r.alone ? each * r.shared : r.alone;
+    const double each = groups <= 256 ? 1 : rounds >= 1 ? r.held : groups / 256, step_time = across * (each * r.shared > r.alone ? each * r.shared : r.alone);
     double time = launch + (rounds <= 1 ? 1 : rounds < 4 ? (double)(long long)(rounds + 0.999) : rounds + 0.5) * (part * step_time + r.ends * (each > 2 ? 2 : each > 1 ? 1.4 : 1));
-    if (splits > 1) time += 4 + (double)p.M * p.N * (8.0 * splits + 2) / 6.5e6;  // the parts' sums there and back, and a launch
+    if (splits > 1) time += 5.5 + (double)p.M * p.N * (8.0 * splits + 2) / 6.5e6;  // the parts' sums there and back, and a launch
     return time;
 }
 

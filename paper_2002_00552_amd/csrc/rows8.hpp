@@ -6,26 +6,38 @@
 
 namespace dwm {
 
-// N (1 to 8) elements from p on as binary32, zeros behind them; p is a multiple of its element's size only.
-template <class T> __device__ __forceinline__ void load_octet(const T* p, int n, float (&f)[8])
+// An octet as it lies in memory.
+template <class T> struct Octet {
+    typename Vector<T, kVec<T>>::type r[8 / kVec<T>];
+};
+
+// n (up to 8) elements from p on, zeros behind them; p is a multiple of its element's size only.
+template <class T> __device__ __forceinline__ Octet<T> fetch_octet(const T* p, int n)
 {
+    Octet<T> o;
     if (n >= 8) {
-        constexpr int V = kVec<T>;
-        typename Vector<T, V>::type r[8 / V];
 #pragma unroll
-        for (int i = 0; i < 8 / V; ++i) r[i] = load_vector<T, V>(p + i * V);
-#pragma unroll
-        for (int i = 0; i < 8 / V; ++i) {
-            float q[V];
-            unpack<T, V>(r[i], q);
-#pragma unroll
-            for (int j = 0; j < V; ++j) f[i * V + j] = q[j];
-        }
+        for (int i = 0; i < 8 / kVec<T>; ++i) o.r[i] = load_vector<T, kVec<T>>(p + i * kVec<T>);
     } else {
+        T t[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = j < n ? (float)p[j] : 0.0f;
+        for (int j = 0; j < 8; ++j) t[j] = j < n ? p[j] : (T)0.0f;
+        __builtin_memcpy(&o, t, sizeof(o));
+    }
+    return o;
+}
+template <class T> __device__ __forceinline__ void octet_values(const Octet<T>& o, float (&f)[8])
+{
+    constexpr int V = kVec<T>;
+#pragma unroll
+    for (int i = 0; i < 8 / V; ++i) {
+        float q[V];
+        unpack<T, V>(o.r[i], q);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[i * V + j] = q[j];
     }
 }
+template <class T> __device__ __forceinline__ void load_octet(const T* p, int n, float (&f)[8]) { octet_values<T>(fetch_octet<T>(p, n), f); }
 
 template <class T> __device__ __forceinline__ void store_octet(T* p, int n, const float (&f)[8])
 {

@@ -127,22 +127,38 @@ def test_sums_in_place():
 
 def test_no_value_of_another_row_gets_in():
     """NaN in the rows and terms around the operands, and in one row of a: it spoils that row alone."""
-    M, N, K = 70, 90, 100
-    for operands in ("f16", "bf16"):
-        for flags in LAYOUTS:
-            for wide in (0, 4, 11):
-                av, bv = normal(M, K, 1), normal(N, K, 2)
-                a = Rows(*((K, M) if flags & 1 else (M, K)), operands, wide, 0)
-                b = Rows(*((K, N) if flags & 2 else (N, K)), operands, wide, 0)
-                a.buffer.fill_(float("nan"))
-                b.buffer.fill_(float("nan"))
-                av[5, 3] = np.nan
-                a.view.copy_(torch.from_numpy(av.T if flags & 1 else av))
-                b.view.copy_(torch.from_numpy(bv.T if flags & 2 else bv))
-                out = Rows(M, N, operands)
-                plan = Plan("matmul", M, N, K, TYPE[operands], TYPE[operands], dwm.DWM_F32, 0, flags, strides={"a": a, "b": b})
-                dwm.dwm_matmul(plan.plan, a.ptr(), b.ptr(), None, None, out.ptr(), None, None, stream())
-                torch.cuda.synchronize()
-                bad = np.isnan(out.numpy())
-                assert bad[5].all() and not np.delete(bad, 5, axis=0).any()
-                plan.close()
+    for M, N, K in ((70, 90, 100), (20, 90, 100), (3, 40, 72)):
+        for operands in ("f16", "bf16"):
+            for flags in LAYOUTS:
+                for wide in (0, 4, 8, 11):
+                    av, bv = normal(M, K, 1), normal(N, K, 2)
+                    a = Rows(*((K, M) if flags & 1 else (M, K)), operands, wide, 0)
+                    b = Rows(*((K, N) if flags & 2 else (N, K)), operands, wide, 0)
+                    a.buffer.fill_(float("nan"))
+                    b.buffer.fill_(float("nan"))
+                    av[1, 3] = np.nan
+                    a.view.copy_(torch.from_numpy(av.T if flags & 1 else av))
+                    b.view.copy_(torch.from_numpy(bv.T if flags & 2 else bv))
+                    out = Rows(M, N, operands)
+                    plan = Plan("matmul", M, N, K, TYPE[operands], TYPE[operands], dwm.DWM_F32, 0, flags, strides={"a": a, "b": b})
+                    dwm.dwm_matmul(plan.plan, a.ptr(), b.ptr(), None, None, out.ptr(), None, None, stream())
+                    torch.cuda.synchronize()
+                    bad = np.isnan(out.numpy())
+                    assert bad[1].all() and not np.delete(bad, 1, axis=0).any()
+                    plan.close()
+
+
+@pytest.mark.parametrize("kernel, M", [(2, 40), (3, 40), (4, 40), (5, 20)])
+def test_codes_of_nan(kernel, M):
+    """An infinity or NaN that was packed spoils its own row of the result, as a row of b its own column."""
+    N, K = 70, 200
+    av, bv = normal(M, K, 1), normal(N, K, 2)
+    av[4, 199], bv[60, 0] = np.inf, np.nan
+    a, b, out = PackedRows(M, K, av), PackedRows(N, K, bv), Rows(M, N, "bf16")
+    plan = Plan("matmul", M, N, K, dwm.DWM_PACKED, dwm.DWM_BF16, dwm.DWM_F32, 0, 0, variants={"kernel": kernel})
+    dwm.dwm_matmul_packed(plan.plan, a.t, b.t, None, None, out.ptr(), None, None, stream())
+    torch.cuda.synchronize()
+    want = np.zeros((M, N), bool)
+    want[4], want[:, 60] = True, True
+    assert np.array_equal(np.isnan(out.numpy()), want)
+    plan.close()
