@@ -75,6 +75,14 @@ __device__ __forceinline__ Rstd rms_rstd(double sum, const RmsArgs& a)
     return {hi, hi < 3e38f ? (float)(r - (double)hi) : 0.0f};
 }
 
+// Whether a number lies right between two codes, or is the largest that a scale holds: one in some 2^20 does once it is rounded to binary32, which side the
+// exact value is on then decides, and not the tie.
+__device__ __forceinline__ bool on_border(float y)
+{
+    const uint32_t u = __float_as_uint(y);
+    return (u & 0xfffffu) == 0x80000u || (u & 0x7fffffu) == 0x600000u;
+}
+
 // What a row's octet leaves behind: z, y and both in 8 bits.
 template <class T>
 __device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int octet, const float (&z)[8], const float (&gamma)[8], Rstd rstd)
@@ -87,17 +95,27 @@ __device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int o
         store_packed(a.kept, row, octet, a.C, codes, s);
     }
     if (!a.y && !a.packed_y.codes) return;
-    float y[8];
+    float y[8], t[8], rest[8];  // y = t * hi + rest, t * hi rounded with it: one rounding
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {  // one rounding: the product's rest and rstd's go in before it
-        const float t = z[j] * gamma[j], rest = fmaf(z[j], gamma[j], -t);
-        y[j] = fmaf(t, rstd.hi, fmaf(t, rstd.lo, rest * rstd.hi));
+    for (int j = 0; j < 8; ++j) {
+        t[j] = z[j] * gamma[j];
+        rest[j] = fmaf(t[j], rstd.lo, fmaf(z[j], gamma[j], -t[j]) * rstd.hi);
+        y[j] = fmaf(t[j], rstd.hi, rest[j]);
     }
     if (a.y && n > 0) store_octet<T>((T*)a.y + row * a.stride[kRmsY] + c, n, y);
     if (a.packed_y.codes) {
         if (n < 8)
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = j < n ? y[j] : 0.0f;  // (an infinite rstd makes NaN of zeros)
+        bool border = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) border |= on_border(y[j]);
+        if (border)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float off = fmaf(t[j], rstd.hi, -y[j]) + rest[j];
+                if (j < n && on_border(y[j]) && off != 0.0f) y[j] = __uint_as_float(__float_as_uint(y[j]) + ((off > 0.0f) == (y[j] > 0.0f) ? 1 : -1));
+            }
         uint32_t s;
         const uint2v codes = pack_octet<QuadLanes>(y, &s);
         store_packed(a.packed_y, row, octet, a.C, codes, s);
