@@ -1,6 +1,8 @@
 // Activations with a bias, their checkpoints in 8 bits and their gradients from them, rows into 8 bits and back; the last sums of
 // the parameters' gradients (gfx950).  Memory bounds all but the gelus in 16 bits, where the vector units come near it: an octet of
-// neighbouring channels to a thread.  A workgroup's 256 threads lie along one row or along several short ones.
+// neighbouring channels to a thread, one row at a time and as many waves as a CU holds (four rows at a time, with their loads together and half the waves: 148 us
+// for 136, 199 for 159).  A workgroup's 256 threads lie along one row or along several short ones.  16384 rows of 8192 bfloat16 with a bias and
+// checkpoints, out of the caches: gelu 136 us (5.0 TB/s), its gradient 150 (4.5) and 8 for the last sums; relu 117 and 136; to 8 bits and back 77 and 78 us (5.3 TB/s).
 #include "rows8.hpp"
 
 namespace dwm {

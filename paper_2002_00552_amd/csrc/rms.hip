@@ -1,7 +1,8 @@
 // Root-mean-square norms of rows with the addition of a residual (gfx950).  Memory bounds them: a row is read once and held in registers, an
 // octet of neighbouring channels to a thread (and one to three more, a row's threads further on), so that four lanes hold a block of
 // 32 channels and its scale comes out of two exchanges between neighbours.  A row's threads are a part of a wave, a wave or a
-// workgroup; the kernels for any size read a row twice.
+// workgroup; the kernels for any size read a row twice.  Operands out of the caches, 16384 rows of 4096 bfloat16: z and y from x and residual 99 us (5.4 TB/s), the
+// gradient from z's checkpoint with dz and dgamma 85 us (5.5 TB/s) and 5 for the last sums; a copy of 1 GiB runs at 5.1 TB/s on the same card.
 #include "norm_device.hpp"
 #include "rows8.hpp"
 
@@ -133,17 +134,34 @@ template <class T, int TPR, int K> __global__ __launch_bounds__(rms_threads(TPR)
         const int c = (lane + k * TPR) * 8;
         param_octet<T>(a.gamma, a.param_typed, c, a.C - c, 1.0f, gamma[k]);
     }
-    int turn = 0;
-    for (long long first = (long long)blockIdx.x * R; first < a.rows; first += (long long)gridDim.x * R, ++turn) {
-        const long long row = first + threadIdx.x / TPR;
+    // With one octet a thread and several rows to a workgroup, a row ahead of the one that is worked on.
+    struct Row {
+        Octet<T> x[K], r[K];
+    } ahead;
+    const long long group = threadIdx.x / TPR, step = (long long)gridDim.x * R;
+    const auto fetch = [&](long long row) {
         const bool here = row < a.rows;
-        float z[K][8], r[K][8];
+        if (!here) row = 0;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = (lane + k * TPR) * 8, n = here ? a.C - c : 0;
-            load_octet<T>((const T*)a.x + (here ? row : 0) * a.stride[kRmsX] + c, n, z[k]);
-            if (a.residual) load_octet<T>((const T*)a.residual + (here ? row : 0) * a.stride[kRmsResidual] + c, n, r[k]);
+            ahead.x[k] = fetch_octet<T>((const T*)a.x + row * a.stride[kRmsX] + c, n);
+            if (a.residual) ahead.r[k] = fetch_octet<T>((const T*)a.residual + row * a.stride[kRmsResidual] + c, n);
         }
+    };
+    int turn = 0;
+    if (K == 1) fetch((long long)blockIdx.x * R + group);
+    for (long long first = (long long)blockIdx.x * R; first < a.rows; first += step, ++turn) {
+        const long long row = first + group;
+        const bool here = row < a.rows;
+        if (K > 1) fetch(row);
+        float z[K][8], r[K][8];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            octet_values<T>(ahead.x[k], z[k]);
+            if (a.residual) octet_values<T>(ahead.r[k], r[k]);
+        }
+        if (K == 1 && first + step < a.rows) fetch(row + step);
         if (a.residual)
 #pragma unroll
             for (int k = 0; k < K; ++k) joined<T>(z[k], r[k]);
@@ -376,11 +394,14 @@ template <class T> __global__ __launch_bounds__(256) void rms_gamma_any_kernel(R
 
 constexpr long long kRmsBlocks = 1 << 20;  // of a launch forward, at most
 
+// Forward, a workgroup for each row (or each few short ones), or, from four times the 256 * 1024 threads on that backward kernels have too, so many that go
+// on to further rows, one ahead.  us, operands out of the caches, one workgroup a row and staying: 4096 rows of 4096 bfloat16, z and y, 32.9, 28.1; 16384 rows 114, 99; 5000 of
+// 8192 71, 62; 32768 of 1024 binary32 96, 102 (twice the bytes under way as it is: not there).
 template <class T, int TPR, int K> static dwm_status_t forward_shape(const RmsArgs& a, hipStream_t s)
 {
-    constexpr int R = rms_threads(TPR) / TPR;
-    const long long blocks = (a.rows + R - 1) / R;
-    hipLaunchKernelGGL((rms_forward_kernel<T, TPR, K>), dim3((unsigned)(blocks < kRmsBlocks ? blocks : kRmsBlocks)), dim3(rms_threads(TPR)), 0, s, a);
+    constexpr int R = rms_threads(TPR) / TPR, kStaying = 256 * 1024 / rms_threads(TPR);
+    const long long blocks = (a.rows + R - 1) / R, most = K == 1 && sizeof(T) == 2 && blocks >= 4 * kStaying ? kStaying : kRmsBlocks;
+    hipLaunchKernelGGL((rms_forward_kernel<T, TPR, K>), dim3((unsigned)(blocks < most ? blocks : most)), dim3(rms_threads(TPR)), 0, s, a);
     return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
 }
 template <class T, int TPR, int K> static dwm_status_t backward_shape(const RmsArgs& a, hipStream_t s)
