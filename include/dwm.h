@@ -663,14 +663,14 @@ typedef struct {
 } dwm_matmul_info_t;
 
 /* operands: DWM_F16 or DWM_BF16, with type (that of out and residual) the same or DWM_F32; or DWM_PACKED, with type DWM_F16 or
- * DWM_BF16 and flags 0.  param_type (of bias) is DWM_F32 or the 16-bit one of the two types.  M, N >= 0 (0: nothing to do), K >= 0 (0: p = bias).  DWM_ERR_UNSUPPORTED for M, N or K above
+ * DWM_BF16 and flags 0.  param_type (of bias) is DWM_F32, or the operands' 16-bit type (packed operands: type).  M, N >= 0 (0: nothing to do), K >= 0 (0: p = bias).  DWM_ERR_UNSUPPORTED for M, N or K above
  * 2^24, M * N above 2^37, or other types.  Host only. */
 DWM_API dwm_status_t dwm_matmul_plan_create(dwm_matmul_plan_t** out, int M, int N, int K, dwm_type_t operands, dwm_type_t type,
                                             dwm_type_t param_type, dwm_act_t act, int flags);
 DWM_API dwm_status_t dwm_matmul_plan_destroy(dwm_matmul_plan_t* plan);
 DWM_API dwm_status_t dwm_matmul_plan_info(const dwm_matmul_plan_t* plan, dwm_matmul_info_t* info);
-/* Elements between rows of "a", "b" (16-bit operands), "residual" or "out".  At any time.  16-bit operands whose address is a multiple of 16 and
- * whose stride and row length are multiples of 8 take the faster kernels. */
+/* Elements between rows of "a", "b" (16-bit operands), "residual" or "out".  At any time.  16-bit operands whose address is a multiple of 16,
+ * whose stride and row length are multiples of 8 and whose stride is at most 2^22 take the faster kernels. */
 DWM_API dwm_status_t dwm_matmul_set_stride(dwm_matmul_plan_t* plan, const char* tensor, long long stride);
 /* For tuning and tests, before dwm_matmul_set_workspace only (DWM_ERR_WORKSPACE afterwards): "kernel": tiles of 128 x 128 (0) or 64 x 64 (1) of
  * the result for operands of any alignment, not built for packed ones; 64 x 64 (2), 128 x 128 (3), 256 x 256 (4) for aligned ones; 5 = few rows
@@ -684,7 +684,8 @@ DWM_API dwm_status_t dwm_matmul_set_workspace(dwm_matmul_plan_t* plan, void* ws_
 DWM_API dwm_status_t dwm_matmul(const dwm_matmul_plan_t* plan, const void* a_dev, const void* b_dev, const void* bias_dev,
                                 const void* residual_dev, void* out_dev, const dwm_packed_t* y_packed, const dwm_packed_t* kept,
                                 void* stream);
-/* The same with a [M][K] and b [N][K] packed (dwm_pack, y_packed of a norm or of another product). */
+/* The same with a [M][K] and b [N][K] packed (dwm_pack, y_packed of a norm or of another product).  The 8-bit matrix cores cut off what lies some 2^-22
+ * below the largest of 128 products before they add them up in binary32: a sum is off by about 1e-5 of the root of its products' summed squares, whatever K is. */
 DWM_API dwm_status_t dwm_matmul_packed(const dwm_matmul_plan_t* plan, const dwm_packed_t* a, const dwm_packed_t* b,
                                        const void* bias_dev, const void* residual_dev, void* out_dev, const dwm_packed_t* y_packed,
                                        const dwm_packed_t* kept, void* stream);

@@ -76,10 +76,10 @@ struct MatmulRate {
 };
 const MatmulRate kMatmulRates[] = {
     {128, 1.8, 1.0, 2, 3.5},   // any alignment (2000 x 2001 x 2003: 48 us in one part, 44 in two, with 64 x 64 tiles 54)
-    {64, 0.8, 0.4, 4, 1.5},    // any alignment (1000 x 777 x 1021: 16 us, with 128 x 128 tiles 23)
-    {64, 0.32, 0.17, 2, 1.5},  // 512 x 512 x 16384: 93 us, in eight parts 22; 1024 x 1024 x 1024: 8, with 128 x 128 tiles 12
+    {64, 0.8, 0.4, 4, 1.5},    // any alignment (1000 x 777 x 1021: 16 us, with 128 x 128 tiles 33)
+    {64, 0.32, 0.17, 2, 1.5},  // 512 x 512 x 16384: 60 us, in eight parts 22, with 128 x 128 tiles 156, 30; 1024 x 1024 x 1024: 8, 15
     {128, 0.68, 0.47, 2, 3.5}, // 2048 x 4096 x 1024: 20 us, with 64 x 64 tiles 31, with 256 x 256 29
-    {256, 1.2, 1.5, 1, 8.0},   // 2048 x 8192 x 2048: 58 us, with 128 x 128 tiles 67
+    {256, 1.2, 1.5, 1, 8.0},   // 2048 x 8192 x 2048: 58 us, with 128 x 128 tiles 70
 };
 
 double matmul_cost(const dwm_matmul_plan& p, int kernel, int splits)

@@ -100,6 +100,7 @@ def test_few_rows(operands, M):
         check(M, N, K, operands, act="gelu", packed=True, wide=8, variants={"kernel": 5})
         check(M, N, K, operands, residual=False, variants={"kernel": 5})
     check(M, 130, 1021, operands, wide=3, off=1)
+    check(M, 33, 1021, operands, wide=3, off=1, packed=True, variants={"kernel": 5})
     check(M, 64, 0, operands, variants={"kernel": 5})
     check(M, 16400, 72, operands, variants={"kernel": 5})
 
