@@ -676,7 +676,8 @@ DWM_API dwm_status_t dwm_matmul_set_stride(dwm_matmul_plan_t* plan, const char* 
  * the result for operands of any alignment, not built for packed ones; 64 x 64 (2), 128 x 128 (3), 256 x 256 (4) for aligned ones; 5 = few rows
  * (M <= 32, neither operand across; never more than one part of K).  "splits": 1 .. 64.  Negative: the planner's choice.  DWM_ERR_INVALID_ARG for what does not apply. */
 DWM_API dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, int variant);
-/* Sums of the parts of K: 256-byte aligned; 0 bytes: not needed. */
+/* Sums of the parts of K, and copies of 16-bit operands whose rows are no multiple of eight elements long, where they pay: 256-byte aligned; 0 bytes: not
+ * needed. */
 DWM_API size_t dwm_matmul_workspace_bytes(const dwm_matmul_plan_t* plan);
 DWM_API dwm_status_t dwm_matmul_set_workspace(dwm_matmul_plan_t* plan, void* ws_dev, size_t bytes);
 /* 16-bit operands.  bias and residual may be NULL; any of out, y_packed (act(p) + residual in 8 bits, from binary32) and kept (p in 8

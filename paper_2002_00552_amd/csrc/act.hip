@@ -155,6 +155,26 @@ dwm_status_t launch_act_backward(const ActArgs& a, dwm_type_t type, void* stream
     }
 }
 
+// An octet to a thread; rows of a product's operand that lie anywhere.
+__global__ __launch_bounds__(256) void aligned_rows_kernel(const _Float16* from, long long stride, _Float16* to, long long to_stride, long long rows, int width)
+{
+    const int octets = (int)(to_stride / 8);
+    const long long total = rows * octets;
+    for (long long at = (long long)blockIdx.x * 256 + threadIdx.x; at < total; at += (long long)gridDim.x * 256) {
+        const long long row = at / octets;
+        const int c = (int)(at - row * octets) * 8;
+        *(uint4v*)(to + row * to_stride + c) = fetch_octet<_Float16>(from + row * stride + c, width - c).r[0];  // (bits, not numbers)
+    }
+}
+
+dwm_status_t launch_aligned_rows(const void* from, long long stride, void* to, long long to_stride, long long rows, int width, void* stream)
+{
+    const long long blocks = (rows * (to_stride / 8) + 255) / 256;
+    hipLaunchKernelGGL(aligned_rows_kernel, dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), 0, (hipStream_t)stream, (const _Float16*)from, stride, (_Float16*)to, to_stride,
+                       rows, width);
+    return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
+}
+
 dwm_status_t launch_columns(const float* partial, int splits, int C, void* out, dwm_type_t type, void* stream)
 {
     const hipStream_t s = (hipStream_t)stream;

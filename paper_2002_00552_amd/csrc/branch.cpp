@@ -75,8 +75,8 @@ struct MatmulRate {
     double ends;
 };
 const MatmulRate kMatmulRates[] = {
-    {128, 1.8, 1.0, 2, 3.5},   // any alignment (2000 x 2001 x 2003: 48 us in one part, 44 in two, with 64 x 64 tiles 54)
-    {64, 0.8, 0.4, 4, 1.5},    // any alignment (1000 x 777 x 1021: 16 us, with 128 x 128 tiles 33)
+    {128, 1.9, 1.3, 2, 3.5},   // any alignment (4001 x 4003 x 4005: 351 us, with 64 x 64 tiles 365; 2000 x 2001 x 2003: 63, 54)
+    {64, 0.8, 0.35, 4, 1.5},   // any alignment (1000 x 777 x 1021: 16 us, with 128 x 128 tiles 34; both across 22, 64)
     {64, 0.32, 0.17, 2, 1.5},  // 512 x 512 x 16384: 60 us, in eight parts 22, with 128 x 128 tiles 156, 30; 1024 x 1024 x 1024: 8, 15
     {128, 0.68, 0.47, 2, 3.5}, // 2048 x 4096 x 1024: 20 us, with 64 x 64 tiles 31, with 256 x 256 29
     {256, 1.2, 1.5, 1, 8.0},   // 2048 x 8192 x 2048: 58 us, with 128 x 128 tiles 70
@@ -89,8 +89,8 @@ double matmul_cost(const dwm_matmul_plan& p, int kernel, int splits)
         return launch + elements * 1e-6 * ((p.operands == DWM_PACKED ? 0.2 : 0.33) + 0.011 * p.M);
     const MatmulRate& r = kMatmulRates[kernel];
     const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step, part = (steps + splits - 1) / splits;
-    const bool reads_across = kernel == kMat64 || kernel == kMat128;  // (twice as many LDS reads, and strides of whole rows)
-    const double across = 1 + (reads_across ? 0.15 * (!!(p.flags & DWM_A_ACROSS) + !!(p.flags & DWM_B_ACROSS)) : 0);
+    const double more = kernel == kMatAny ? 0.4 : kernel < kMat256 ? 0.15 : 0;  // (twice as many LDS reads, and strides of whole rows)
+    const double across = 1 + more * (!!(p.flags & DWM_A_ACROSS) + !!(p.flags & DWM_B_ACROSS));
     const double groups = (double)((p.M + r.side - 1) / r.side) * ((p.N + r.side - 1) / r.side) * splits, rounds = groups / (256.0 * r.held);
     const double each = groups <= 256 ? 1 : rounds >= 1 ? r.held : groups / 256, step_time = across * (each * r.shared > r.alone ? each * r.shared : r.alone);
     double time = launch + (rounds <= 1 ? 1 : rounds < 4 ? (double)(long long)(rounds + 0.999) : rounds + 0.5) * (part * step_time + r.ends * (each > 2 ? 2 : each > 1 ? 1.4 : 1));
@@ -123,6 +123,36 @@ MatmulShape matmul_shape(const dwm_matmul_plan& p, int first, int last, int spli
     return best;
 }
 
+// An operand of 16 bits: its rows, their length, and whether that keeps it from being read sixteen bytes at a time wherever it lies.
+struct OperandRows {
+    long long rows, length;
+    bool odd() const { return length % 8 != 0; }
+    long long stride() const { return (length + 7) / 8 * 8; }  // of a copy
+    size_t bytes() const { return odd() ? (size_t)(rows * stride() * 2 + 255) / 256 * 256 : 0; }
+};
+OperandRows operand_rows(const dwm_matmul_plan& p, bool second)
+{
+    const bool across = p.flags & (second ? DWM_B_ACROSS : DWM_A_ACROSS);
+    const long long own = second ? p.N : p.M;
+    return across ? OperandRows{p.K, own} : OperandRows{own, p.K};
+}
+
+// Laying odd operands out anew: a launch each, and their bytes there and back.
+double copies_cost(const dwm_matmul_plan& p)
+{
+    double time = 0;
+    for (int second = 0; second < 2; ++second) {
+        const OperandRows r = operand_rows(p, second);
+        if (r.odd()) time += 2.5 + (double)r.rows * r.length * 4 / 4.0e6;
+    }
+    return time;
+}
+size_t parts_bytes(const dwm_matmul_plan& p)
+{
+    const int splits = p.shape.splits > p.any.splits ? p.shape.splits : p.any.splits;
+    return splits > 1 ? ((size_t)splits * p.M * matmul_partial_width(p.N) * sizeof(float) + 255) / 256 * 256 : 0;
+}
+
 // kernel, splits: negative for the planner's choice.
 void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
 {
@@ -135,6 +165,11 @@ void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
     } else {
         p.any = matmul_shape(p, kMatAny, kMatAny64, splits);
     }
+    // Rows of odd lengths: the kernels for any alignment, or, where it costs less (or a kernel for aligned operands was asked for), copies and those for aligned ones
+    // (bfloat16, us, without and with: 4001 x 4003 x 4005 351, 144; 1000 x 777 x 1021 16.3, 15.6, both across 21.8, 14.2; 300 x 300 x 500 9.2, 15.0).
+    const OperandRows a = operand_rows(p, false), b = operand_rows(p, true);
+    p.copies = p.operands != DWM_PACKED && (a.odd() || b.odd()) && p.K > 0 && p.shape.kernel >= kMat64 && p.shape.kernel <= kMat256 && a.stride() <= 1 << 22 && b.stride() <= 1 << 22 &&
+               (kernel >= 0 || matmul_cost(p, p.shape.kernel, p.shape.splits) + copies_cost(p) < matmul_cost(p, p.any.kernel, p.any.splits));
 }
 
 // Whether the kernels that copy sixteen bytes at a time straight into LDS can read an operand; a tile's 256 rows have to lie within 2^32 bytes.
@@ -143,11 +178,13 @@ bool operand_aligned(const void* p, long long stride, long long length)
     return aligned(p, 16) && stride % 8 == 0 && length % 8 == 0 && stride <= 1 << 22;
 }
 
-dwm_status_t run_matmul(const dwm_matmul_plan& p, MatmulArgs& a, const MatmulShape& shape, const void* bias, const void* residual,
-                        void* out, const dwm_packed_t* packed_y, const dwm_packed_t* kept, void* stream)
+dwm_status_t run_matmul(const dwm_matmul_plan& p, MatmulArgs& a, const MatmulShape& shape, const long long* strides, const void* bias,
+                        const void* residual, void* out, const dwm_packed_t* packed_y, const dwm_packed_t* kept, void* stream)
 {
     if (shape.splits > 1 && !p.ws) return DWM_ERR_WORKSPACE;
     std::memcpy(a.stride, p.stride, sizeof(a.stride));
+    a.stride[kMatA] = strides[0];
+    a.stride[kMatB] = strides[1];
     a.bias = bias;
     a.residual = residual;
     a.out = out;
@@ -522,9 +559,7 @@ dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, 
 
 size_t dwm_matmul_workspace_bytes(const dwm_matmul_plan_t* plan)
 {
-    if (!plan) return 0;
-    const int splits = plan->shape.splits > plan->any.splits ? plan->shape.splits : plan->any.splits;
-    return splits > 1 ? (size_t)splits * plan->M * matmul_partial_width(plan->N) * sizeof(float) : 0;
+    return plan ? parts_bytes(*plan) + (plan->copies ? operand_rows(*plan, false).bytes() + operand_rows(*plan, true).bytes() : 0) : 0;
 }
 
 dwm_status_t dwm_matmul_set_workspace(dwm_matmul_plan_t* plan, void* ws_dev, size_t bytes)
@@ -545,9 +580,33 @@ dwm_status_t dwm_matmul(const dwm_matmul_plan_t* plan, const void* a_dev, const 
     MatmulArgs a{};
     a.a = a_dev;
     a.b = b_dev;
-    const bool fast = operand_aligned(a_dev, plan->stride[kMatA], plan->flags & DWM_A_ACROSS ? plan->M : plan->K) &&
-                      operand_aligned(b_dev, plan->stride[kMatB], plan->flags & DWM_B_ACROSS ? plan->N : plan->K);
-    return run_matmul(*plan, a, fast ? plan->shape : plan->any, bias_dev, residual_dev, out_dev, y_packed, kept, stream);
+    long long strides[2] = {plan->stride[kMatA], plan->stride[kMatB]};
+    const void* operands[2] = {a_dev, b_dev};
+    if (plan->copies) {  // where the operand that needs no copy can be read as it lies
+        bool good = true;
+        for (int second = 0; second < 2; ++second) {
+            const OperandRows r = operand_rows(*plan, second);
+            good = good && (r.odd() || operand_aligned(operands[second], strides[second], r.length));
+        }
+        if (good) {
+            if (!plan->ws) return DWM_ERR_WORKSPACE;
+            char* to = (char*)plan->ws + parts_bytes(*plan);
+            for (int second = 0; second < 2; ++second) {
+                const OperandRows r = operand_rows(*plan, second);
+                if (!r.odd()) continue;
+                const dwm_status_t st = launch_aligned_rows(operands[second], strides[second], to, r.stride(), r.rows, (int)r.length, stream);
+                if (st != DWM_OK) return st;
+                operands[second] = to;
+                strides[second] = r.stride();
+                to += r.bytes();
+            }
+            a.a = operands[0];
+            a.b = operands[1];
+            return run_matmul(*plan, a, plan->shape, strides, bias_dev, residual_dev, out_dev, y_packed, kept, stream);
+        }
+    }
+    const bool fast = operand_aligned(a_dev, strides[0], operand_rows(*plan, false).length) && operand_aligned(b_dev, strides[1], operand_rows(*plan, true).length);
+    return run_matmul(*plan, a, fast ? plan->shape : plan->any, strides, bias_dev, residual_dev, out_dev, y_packed, kept, stream);
 }
 
 dwm_status_t dwm_matmul_packed(const dwm_matmul_plan_t* plan, const dwm_packed_t* a, const dwm_packed_t* b, const void* bias_dev,
@@ -565,7 +624,7 @@ dwm_status_t dwm_matmul_packed(const dwm_matmul_plan_t* plan, const dwm_packed_t
         args.b = b->codes;
         args.b_scales = (const uint8_t*)b->scales;
     }
-    return run_matmul(*plan, args, plan->shape, bias_dev, residual_dev, out_dev, y_packed, kept, stream);
+    return run_matmul(*plan, args, plan->shape, plan->stride, bias_dev, residual_dev, out_dev, y_packed, kept, stream);
 }
 
 }  // extern "C"

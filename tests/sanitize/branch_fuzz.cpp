@@ -53,6 +53,16 @@ dwm_status_t launch_columns(const float* partial, int splits, int C, void* out, 
     return DWM_OK;
 }
 
+static uintptr_t copies_from = 0, copies_to = 0;  // the workspace that copies have to stay in
+
+dwm_status_t launch_aligned_rows(const void* from, long long stride, void* to, long long to_stride, long long rows, int width, void*)
+{
+    ++launches;
+    require(from && rows > 0 && width > 0 && stride >= width && to_stride >= width && to_stride < width + 8 && to_stride % 8 == 0, "rows to copy");
+    require((uintptr_t)to % 256 == 0 && (uintptr_t)to >= copies_from && (uintptr_t)to + rows * to_stride * 2 <= copies_to, "copies outside the workspace");
+    return DWM_OK;
+}
+
 static dwm_status_t matmul(const MatmulArgs& a, int flags, int kernel, bool packed)
 {
     ++launches;
@@ -60,8 +70,10 @@ static dwm_status_t matmul(const MatmulArgs& a, int flags, int kernel, bool pack
     if (packed) require(kernel >= kMat64 && kernel <= kMatFew, "packed operands and a kernel for any alignment");
     if (kernel >= kMatFew) require(a.M <= kMatFewRows && !flags && a.splits == 1, "few rows");
     if (!packed && a.K > 0 && kernel >= kMat64 && kernel <= kMatFew) {
-        const long long la = flags & DWM_A_ACROSS ? a.M : a.K, lb = flags & DWM_B_ACROSS ? a.N : a.K;
-        require(la % 8 == 0 && lb % 8 == 0 && a.stride[kMatA] % 8 == 0 && a.stride[kMatB] % 8 == 0 && (uintptr_t)a.a % 16 == 0 && (uintptr_t)a.b % 16 == 0, "sixteen bytes at a time");
+        const long long la = flags & DWM_A_ACROSS ? a.M : a.K, lb = flags & DWM_B_ACROSS ? a.N : a.K;  // (rows of odd lengths come as copies, whole vectors apart)
+        require((la + 7) / 8 * 8 <= a.stride[kMatA] && (lb + 7) / 8 * 8 <= a.stride[kMatB] && a.stride[kMatA] % 8 == 0 && a.stride[kMatB] % 8 == 0 && (uintptr_t)a.a % 16 == 0 && (uintptr_t)a.b % 16 == 0,
+                "sixteen bytes at a time");
+        require((la % 8 == 0 || (uintptr_t)a.a > 1 << 20) && (lb % 8 == 0 || (uintptr_t)a.b > 1 << 20), "rows of odd lengths that are no copies");
         require(a.stride[kMatA] * 2 * 256 < 1LL << 32 && a.stride[kMatB] * 2 * 256 < 1LL << 32, "offsets of 32 bits");
     }
     return DWM_OK;
@@ -120,7 +132,10 @@ int main(int argc, char** argv)
             dwm_matmul_info_t info;
             require(dwm_matmul_plan_info(mm, &info) == DWM_OK && info.splits >= 1, "product info");
             const size_t bytes = dwm_matmul_workspace_bytes(mm);
-            if (bytes && upto(3)) require(dwm_matmul_set_workspace(mm, kWs, bytes) == DWM_OK, "product workspace");
+            void* const space = (void*)((uintptr_t)1 << 40);
+            dwm::copies_from = (uintptr_t)space;
+            dwm::copies_to = dwm::copies_from + bytes;
+            if (bytes && upto(3)) require(dwm_matmul_set_workspace(mm, space, bytes) == DWM_OK, "product workspace");
             if (operands == DWM_PACKED)
                 dwm_matmul_packed(mm, &p, &p, nullptr, kWs, kWs, &p, &p, nullptr);
             else

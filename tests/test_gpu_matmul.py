@@ -93,6 +93,17 @@ def test_parts_of_k(operands, kernel):
     check(40, 24, 5000, operands)  # as planned
 
 
+@pytest.mark.parametrize("flags", LAYOUTS)
+@pytest.mark.parametrize("operands", ["f16", "bf16"])
+def test_odd_rows_laid_out_anew(operands, flags):
+    """Kernels for aligned operands asked for where rows are of odd lengths: copies in the workspace, in one and in several parts of K."""
+    for kernel in (2, 3, 4):
+        for M, N, K in ((40, 72, 129), (65, 33, 200), (300, 261, 1021)):
+            check(M, N, K, operands, flags=flags, wide=3, off=1, variants={"kernel": kernel, "splits": 1}, packed=True, act="gelu")
+        check(136, 131, 1003, operands, flags=flags, variants={"kernel": kernel, "splits": 3})
+    check(1030, 1029, 1027, operands, flags=flags, wide=5)  # as planned
+
+
 @pytest.mark.parametrize("M", [1, 2, 15, 16, 17, 31, 32])
 @pytest.mark.parametrize("operands", ["f16", "bf16", "packed"])
 def test_few_rows(operands, M):
