@@ -155,23 +155,27 @@ dwm_status_t launch_act_backward(const ActArgs& a, dwm_type_t type, void* stream
     }
 }
 
-// An octet to a thread; rows of a product's operand that lie anywhere.
-__global__ __launch_bounds__(256) void aligned_rows_kernel(const _Float16* from, long long stride, _Float16* to, long long to_stride, long long rows, int width)
+// An octet to a thread; rows of one or two of a product's operands that lie anywhere.
+__global__ __launch_bounds__(256) void aligned_rows_kernel(AlignedRows first, AlignedRows second)
 {
-    const int octets = (int)(to_stride / 8);
-    const long long total = rows * octets;
+    const AlignedRows& r = blockIdx.y ? second : first;
+    const int octets = (int)(r.to_stride / 8);
+    const long long total = r.rows * octets;
     for (long long at = (long long)blockIdx.x * 256 + threadIdx.x; at < total; at += (long long)gridDim.x * 256) {
         const long long row = at / octets;
         const int c = (int)(at - row * octets) * 8;
-        *(uint4v*)(to + row * to_stride + c) = fetch_octet<_Float16>(from + row * stride + c, width - c).r[0];  // (bits, not numbers)
+        *(uint4v*)((_Float16*)r.to + row * r.to_stride + c) = fetch_octet<_Float16>((const _Float16*)r.from + row * r.stride + c, r.width - c).r[0];  // (bits, not numbers)
     }
 }
 
-dwm_status_t launch_aligned_rows(const void* from, long long stride, void* to, long long to_stride, long long rows, int width, void* stream)
+dwm_status_t launch_aligned_rows(const AlignedRows* r, int count, void* stream)
 {
-    const long long blocks = (rows * (to_stride / 8) + 255) / 256;
-    hipLaunchKernelGGL(aligned_rows_kernel, dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)), dim3(256), 0, (hipStream_t)stream, (const _Float16*)from, stride, (_Float16*)to, to_stride,
-                       rows, width);
+    long long blocks = 1;
+    for (int i = 0; i < count; ++i) {
+        const long long own = (r[i].rows * (r[i].to_stride / 8) + 255) / 256;
+        if (own > blocks) blocks = own;
+    }
+    hipLaunchKernelGGL(aligned_rows_kernel, dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20), (unsigned)count), dim3(256), 0, (hipStream_t)stream, r[0], r[count - 1]);
     return hipGetLastError() == hipSuccess ? DWM_OK : DWM_ERR_HIP;
 }
 

@@ -76,7 +76,7 @@ struct MatmulRate {
 };
 const MatmulRate kMatmulRates[] = {
     {128, 1.9, 1.3, 2, 3.5},   // any alignment (4001 x 4003 x 4005: 351 us, with 64 x 64 tiles 365; 2000 x 2001 x 2003: 63, 54)
-    {64, 0.8, 0.35, 4, 1.5},   // any alignment (1000 x 777 x 1021: 16 us, with 128 x 128 tiles 34; both across 22, 64)
+    {64, 0.7, 0.35, 4, 1.5},   // any alignment (1000 x 777 x 1021: 16 us, with 128 x 128 tiles 34; both across 22, 64)
     {64, 0.32, 0.17, 2, 1.5},  // 512 x 512 x 16384: 60 us, in eight parts 22, with 128 x 128 tiles 156, 30; 1024 x 1024 x 1024: 8, 15
     {128, 0.68, 0.47, 2, 3.5}, // 2048 x 4096 x 1024: 20 us, with 64 x 64 tiles 31, with 256 x 256 29
     {256, 1.2, 1.5, 1, 8.0},   // 2048 x 8192 x 2048: 58 us, with 128 x 128 tiles 70
@@ -89,7 +89,7 @@ double matmul_cost(const dwm_matmul_plan& p, int kernel, int splits)
         return launch + elements * 1e-6 * ((p.operands == DWM_PACKED ? 0.2 : 0.33) + 0.011 * p.M);
     const MatmulRate& r = kMatmulRates[kernel];
     const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step, part = (steps + splits - 1) / splits;
-    const double more = kernel == kMatAny ? 0.4 : kernel < kMat256 ? 0.15 : 0;  // (twice as many LDS reads, and strides of whole rows)
+    const double more = kernel == kMatAny ? 0.4 : kernel == kMatAny64 ? 0.25 : kernel < kMat256 ? 0.15 : 0;  // (twice as many LDS reads, and strides of whole rows)
     const double across = 1 + more * (!!(p.flags & DWM_A_ACROSS) + !!(p.flags & DWM_B_ACROSS));
     const double groups = (double)((p.M + r.side - 1) / r.side) * ((p.N + r.side - 1) / r.side) * splits, rounds = groups / (256.0 * r.held);
     const double each = groups <= 256 ? 1 : rounds >= 1 ? r.held : groups / 256, step_time = across * (each * r.shared > r.alone ? each * r.shared : r.alone);
@@ -137,13 +137,13 @@ OperandRows operand_rows(const dwm_matmul_plan& p, bool second)
     return across ? OperandRows{p.K, own} : OperandRows{own, p.K};
 }
 
-// Laying odd operands out anew: a launch each, and their bytes there and back.
+// Laying odd operands out anew: a launch, and their bytes there and back.
 double copies_cost(const dwm_matmul_plan& p)
 {
-    double time = 0;
+    double time = 4;
     for (int second = 0; second < 2; ++second) {
         const OperandRows r = operand_rows(p, second);
-        if (r.odd()) time += 2.5 + (double)r.rows * r.length * 4 / 4.0e6;
+        if (r.odd()) time += (double)r.rows * r.length * 4 / 4.0e6;
     }
     return time;
 }
@@ -166,7 +166,7 @@ void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
         p.any = matmul_shape(p, kMatAny, kMatAny64, splits);
     }
     // Rows of odd lengths: the kernels for any alignment, or, where it costs less (or a kernel for aligned operands was asked for), copies and those for aligned ones
-    // (bfloat16, us, without and with: 4001 x 4003 x 4005 351, 144; 1000 x 777 x 1021 16.3, 15.6, both across 21.8, 14.2; 300 x 300 x 500 9.2, 15.0).
+    // (bfloat16, us, without and with: 4001 x 4003 x 4005 350, 142; 1000 x 777 x 1021 16.3, 13.6, both across 22.7, 13.9; 300 x 300 x 500 8.3, 12.4).
     const OperandRows a = operand_rows(p, false), b = operand_rows(p, true);
     p.copies = p.operands != DWM_PACKED && (a.odd() || b.odd()) && p.K > 0 && p.shape.kernel >= kMat64 && p.shape.kernel <= kMat256 && a.stride() <= 1 << 22 && b.stride() <= 1 << 22 &&
                (kernel >= 0 || matmul_cost(p, p.shape.kernel, p.shape.splits) + copies_cost(p) < matmul_cost(p, p.any.kernel, p.any.splits));
@@ -591,15 +591,18 @@ dwm_status_t dwm_matmul(const dwm_matmul_plan_t* plan, const void* a_dev, const 
         if (good) {
             if (!plan->ws) return DWM_ERR_WORKSPACE;
             char* to = (char*)plan->ws + parts_bytes(*plan);
+            AlignedRows rows[2];
+            int count = 0;
             for (int second = 0; second < 2; ++second) {
                 const OperandRows r = operand_rows(*plan, second);
                 if (!r.odd()) continue;
-                const dwm_status_t st = launch_aligned_rows(operands[second], strides[second], to, r.stride(), r.rows, (int)r.length, stream);
-                if (st != DWM_OK) return st;
+                rows[count++] = {operands[second], strides[second], to, r.stride(), r.rows, (int)r.length};
                 operands[second] = to;
                 strides[second] = r.stride();
                 to += r.bytes();
             }
+            const dwm_status_t st = launch_aligned_rows(rows, count, stream);
+            if (st != DWM_OK) return st;
             a.a = operands[0];
             a.b = operands[1];
             return run_matmul(*plan, a, plan->shape, strides, bias_dev, residual_dev, out_dev, y_packed, kept, stream);

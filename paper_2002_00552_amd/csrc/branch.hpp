@@ -78,14 +78,22 @@ struct MatmulShape {
 };
 inline long long matmul_partial_width(int N) { return packed_width(N); }
 
+// `rows` rows of `width` 16-bit elements from anywhere to rows of `to_stride` (a multiple of 8, at a multiple of 16 bytes), zeros behind each.
+struct AlignedRows {
+    const void* from;
+    long long stride;
+    void* to;
+    long long to_stride, rows;
+    int width;
+};
+
 dwm_status_t launch_rms_forward(const RmsArgs& a, dwm_type_t type, int kernel, void* stream);
 dwm_status_t launch_rms_backward(const RmsArgs& a, dwm_type_t type, int kernel, void* stream);
 dwm_status_t launch_act_forward(const ActArgs& a, dwm_type_t type, void* stream);
 dwm_status_t launch_act_backward(const ActArgs& a, dwm_type_t type, void* stream);
 // out[c] = sum over the splits of partial[split][c], in the order of the splits.
 dwm_status_t launch_columns(const float* partial, int splits, int C, void* out, dwm_type_t type, void* stream);
-// `rows` rows of `width` 16-bit elements from anywhere to rows of `to_stride` (a multiple of 8, at a multiple of 16 bytes), zeros behind each.
-dwm_status_t launch_aligned_rows(const void* from, long long stride, void* to, long long to_stride, long long rows, int width, void* stream);
+dwm_status_t launch_aligned_rows(const AlignedRows* r, int count, void* stream);  // one or two
 // flags: DWM_A_ACROSS, DWM_B_ACROSS.
 dwm_status_t launch_matmul_f16(const MatmulArgs& a, int flags, int kernel, void* stream);
 dwm_status_t launch_matmul_bf16(const MatmulArgs& a, int flags, int kernel, void* stream);

@@ -55,11 +55,17 @@ dwm_status_t launch_columns(const float* partial, int splits, int C, void* out, 
 
 static uintptr_t copies_from = 0, copies_to = 0;  // the workspace that copies have to stay in
 
-dwm_status_t launch_aligned_rows(const void* from, long long stride, void* to, long long to_stride, long long rows, int width, void*)
+dwm_status_t launch_aligned_rows(const AlignedRows* r, int count, void*)
 {
     ++launches;
-    require(from && rows > 0 && width > 0 && stride >= width && to_stride >= width && to_stride < width + 8 && to_stride % 8 == 0, "rows to copy");
-    require((uintptr_t)to % 256 == 0 && (uintptr_t)to >= copies_from && (uintptr_t)to + rows * to_stride * 2 <= copies_to, "copies outside the workspace");
+    require(count == 1 || count == 2, "operands to copy");
+    for (int i = 0; i < count; ++i) {
+        const uintptr_t to = (uintptr_t)r[i].to, end = to + r[i].rows * r[i].to_stride * 2;
+        require(r[i].from && r[i].rows > 0 && r[i].width > 0 && r[i].stride >= r[i].width, "rows to copy");
+        require(r[i].to_stride >= r[i].width && r[i].to_stride < r[i].width + 8 && r[i].to_stride % 8 == 0, "rows of a copy");
+        require(to % 256 == 0 && to >= copies_from && end <= copies_to, "copies outside the workspace");
+        if (i) require(to >= (uintptr_t)r[0].to + r[0].rows * r[0].to_stride * 2, "copies over each other");
+    }
     return DWM_OK;
 }
 
