@@ -174,3 +174,43 @@ def test_codes_of_nan(kernel, M):
     want[4], want[:, 60] = True, True
     assert np.array_equal(np.isnan(out.numpy()), want)
     plan.close()
+
+
+@pytest.mark.parametrize("flags", LAYOUTS)
+@pytest.mark.parametrize("kernel", [2, 3, 4])
+def test_no_value_of_another_row_gets_into_copies(kernel, flags):
+    """The same where operands of odd rows are laid out anew, eagerly and in a graph replayed over a spoilt workspace."""
+    for M, N, K, wide, splits in ((70, 91, 101, 5, 1), (72, 88, 101, 8, 1), (71, 96, 328, 8, 1), (300, 261, 1021, 3, 2)):
+        print("matmul copies", M, N, K, wide, splits, flush=True)
+        av, bv = normal(M, K, 1), normal(N, K, 2)
+        a = Rows(*((K, M) if flags & 1 else (M, K)), "bf16", wide, 0)
+        b = Rows(*((K, N) if flags & 2 else (N, K)), "bf16", wide, 0)
+        a.buffer.fill_(float("nan"))
+        b.buffer.fill_(float("nan"))
+        if wide == 8:  # the operand of whole vectors begins at a multiple of sixteen bytes
+            a.view, b.view = (t.buffer[:t.rows * t.stride].view(t.rows, t.stride)[:, :t.C] for t in (a, b))
+        av[1, 3] = np.nan
+        a.view.copy_(torch.from_numpy(av.T if flags & 1 else av))
+        b.view.copy_(torch.from_numpy(bv.T if flags & 2 else bv))
+        out = Rows(M, N, "bf16")
+        plan = Plan("matmul", M, N, K, TYPE["bf16"], TYPE["bf16"], dwm.DWM_F32, 0, flags, strides={"a": a, "b": b}, variants={"kernel": kernel, "splits": splits})
+        try:
+            def run():
+                dwm.dwm_matmul(plan.plan, a.ptr(), b.ptr(), None, None, out.ptr(), None, None, stream())
+
+            run()
+            torch.cuda.synchronize()
+            first = out.view.clone()
+            bad = np.isnan(out.numpy())
+            assert bad[1].all() and not np.delete(bad, 1, axis=0).any()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                run()
+            for _ in range(3):
+                plan.ws.fill_(float("nan"))
+                out.view.fill_(3.0)
+                graph.replay()
+                torch.cuda.synchronize()
+                assert torch.equal(out.view.view(torch.int16), first.view(torch.int16))
+        finally:
+            plan.close()
