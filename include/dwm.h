@@ -674,7 +674,8 @@ DWM_API dwm_status_t dwm_matmul_plan_info(const dwm_matmul_plan_t* plan, dwm_mat
 DWM_API dwm_status_t dwm_matmul_set_stride(dwm_matmul_plan_t* plan, const char* tensor, long long stride);
 /* For tuning and tests, before dwm_matmul_set_workspace only (DWM_ERR_WORKSPACE afterwards): "kernel": tiles of 128 x 128 (0) or 64 x 64 (1) of
  * the result for operands of any alignment, not built for packed ones; 64 x 64 (2), 128 x 128 (3), 256 x 256 (4) for aligned ones (rows of odd lengths are copied first); 5 = few rows
- * (M <= 32, neither operand across; never more than one part of K).  "splits": 1 .. 64.  Negative: the planner's choice.  DWM_ERR_INVALID_ARG for what does not apply. */
+ * (M <= 32, neither operand across; never more than one part of K).  "splits": 1 .. 64, with the kernel that was asked for, or else the one that the planner takes with so many; "kernel" takes
+ * it back.  Negative: the planner's choice.  DWM_ERR_INVALID_ARG for what does not apply. */
 DWM_API dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, int variant);
 /* Sums of the parts of K, and copies of 16-bit operands whose rows are no multiple of eight elements long, where they pay: 256-byte aligned; 0 bytes: not
  * needed. */

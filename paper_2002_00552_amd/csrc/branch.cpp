@@ -509,6 +509,7 @@ dwm_status_t dwm_matmul_plan_create(dwm_matmul_plan_t** out, int M, int N, int K
     p->stride[kMatA] = flags & DWM_A_ACROSS ? M : K;
     p->stride[kMatB] = flags & DWM_B_ACROSS ? N : K;
     p->stride[kMatResidual] = p->stride[kMatOut] = N;
+    p->asked_kernel = -1;
     matmul_plan(*p, -1, -1);
     *out = p;
     return DWM_OK;
@@ -549,10 +550,11 @@ dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, 
     if (plan->ws) return DWM_ERR_WORKSPACE;
     if (kernel) {
         if (variant >= 0 && !matmul_applies(*plan, variant)) return DWM_ERR_INVALID_ARG;
-        matmul_plan(*plan, variant < 0 ? -1 : variant, -1);
+        plan->asked_kernel = variant < 0 ? -1 : variant;
+        matmul_plan(*plan, plan->asked_kernel, -1);
     } else {
-        if (variant == 0 || variant > 64 || (variant > 1 && plan->shape.kernel == kMatFew)) return DWM_ERR_INVALID_ARG;
-        matmul_plan(*plan, plan->shape.kernel, variant);
+        if (variant == 0 || variant > 64 || (variant > 1 && plan->asked_kernel == kMatFew)) return DWM_ERR_INVALID_ARG;
+        matmul_plan(*plan, plan->asked_kernel, variant);
     }
     return DWM_OK;
 }

@@ -126,6 +126,7 @@ struct dwm_matmul_plan {
     dwm_type_t operands, type, param_type;
     dwm_act_t act;
     long long stride[dwm::kMatTensors];
+    int asked_kernel;        // by dwm_matmul_set_variant; negative: the planner's choice
     dwm::MatmulShape shape;  // where the operands are aligned
     dwm::MatmulShape any;    // and where they are not
     bool copies;             // operands whose rows are no multiple of eight elements are laid out anew first, and `shape` runs
