@@ -658,7 +658,7 @@ enum {
 typedef struct dwm_matmul_plan dwm_matmul_plan_t;
 typedef struct {
     int M, N, K;
-    int kernel; /* dwm_matmul_set_variant's numbers: what runs where the operands, or copies of them, are aligned */
+    int kernel; /* dwm_matmul_set_variant's numbers: what runs where the operands, or copies of them, are aligned; with rows of odd lengths and no copies, what runs */
     int splits; /* parts of K whose products are added up last */
 } dwm_matmul_info_t;
 

@@ -170,6 +170,7 @@ void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
     const OperandRows a = operand_rows(p, false), b = operand_rows(p, true);
     p.copies = p.operands != DWM_PACKED && (a.odd() || b.odd()) && p.K > 0 && p.shape.kernel >= kMat64 && p.shape.kernel <= kMat256 && a.stride() <= 1 << 22 && b.stride() <= 1 << 22 &&
                (kernel >= 0 || matmul_cost(p, p.shape.kernel, p.shape.splits) + copies_cost(p) < matmul_cost(p, p.any.kernel, p.any.splits));
+    if (p.operands != DWM_PACKED && (a.odd() || b.odd()) && p.K > 0 && !p.copies) p.shape = p.any;  // (no address or stride makes these whole vectors)
 }
 
 // Whether the kernels that copy sixteen bytes at a time straight into LDS can read an operand; a tile's 256 rows have to lie within 2^32 bytes.
@@ -525,7 +526,7 @@ dwm_status_t dwm_matmul_plan_destroy(dwm_matmul_plan_t* plan)
 dwm_status_t dwm_matmul_plan_info(const dwm_matmul_plan_t* plan, dwm_matmul_info_t* info)
 {
     if (!plan || !info) return DWM_ERR_INVALID_ARG;
-    *info = dwm_matmul_info_t{plan->M, plan->N, plan->K, plan->shape.kernel, plan->shape.splits};
+    *info = dwm_matmul_info_t{plan->M, plan->N, plan->K, plan->shape.kernel == kMatFewLoose ? (int)kMatFew : plan->shape.kernel, plan->shape.splits};
     return DWM_OK;
 }
 
@@ -610,7 +611,7 @@ dwm_status_t dwm_matmul(const dwm_matmul_plan_t* plan, const void* a_dev, const 
             return run_matmul(*plan, a, plan->shape, strides, bias_dev, residual_dev, out_dev, y_packed, kept, stream);
         }
     }
-    const bool fast = operand_aligned(a_dev, strides[0], operand_rows(*plan, false).length) && operand_aligned(b_dev, strides[1], operand_rows(*plan, true).length);
+    const bool fast = plan->K == 0 || (operand_aligned(a_dev, strides[0], operand_rows(*plan, false).length) && operand_aligned(b_dev, strides[1], operand_rows(*plan, true).length));
     return run_matmul(*plan, a, fast ? plan->shape : plan->any, strides, bias_dev, residual_dev, out_dev, y_packed, kept, stream);
 }
 
