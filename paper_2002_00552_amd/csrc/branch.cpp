@@ -104,16 +104,25 @@ bool matmul_applies(const dwm_matmul_plan& p, int kernel)
     return kernel <= kMatAny64 ? kernel >= 0 && p.operands != DWM_PACKED : kernel < kMatFew;
 }
 
-// The cheapest of some kernels, with as many parts of K as are asked for or the best number of them, each of four steps at least.
+// Whether a launch can hold a workgroup for each tile and part: fewer than 2^32 threads (results of 2^36 elements on in tiles of 64 x 64; one part in larger ones always).
+bool matmul_launches(const dwm_matmul_plan& p, int kernel, int splits)
+{
+    if (kernel >= kMatFew) return true;
+    const long long side = kMatmulRates[kernel].side;
+    return (p.M + side - 1) / side * ((p.N + side - 1) / side) * splits * (side == 256 ? 512 : 256) < 1LL << 32;
+}
+
+// The cheapest of some kernels, with as many parts of K as are asked for or the best number of them, each of four steps at least; kernel -1 where none can be launched.
 MatmulShape matmul_shape(const dwm_matmul_plan& p, int first, int last, int splits)
 {
-    MatmulShape best = {first, splits > 0 && first < kMatFew ? splits : 1};
+    MatmulShape best = {-1, 1};
     double least = -1;
     const long long step = p.operands == DWM_PACKED ? 128 : 64, steps = (p.K + step - 1) / step;
     for (int kernel = first; kernel <= last; ++kernel)
         for (int s = 1; s <= 16; s *= 2) {
             if (s > 1 && (kernel >= kMatFew || splits > 0 || s * 4 > steps)) continue;
             const int parts = splits > 0 && kernel < kMatFew ? splits : s;
+            if (!matmul_launches(p, kernel, parts)) continue;
             const double cost = matmul_cost(p, kernel, parts);
             if (least < 0 || cost < least) {
                 least = cost;
@@ -153,17 +162,20 @@ size_t parts_bytes(const dwm_matmul_plan& p)
     return splits > 1 ? ((size_t)splits * p.M * matmul_partial_width(p.N) * sizeof(float) + 255) / 256 * 256 : 0;
 }
 
-// kernel, splits: negative for the planner's choice.
-void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
+// kernel, splits: negative for the planner's choice.  False, and the plan as it was, for what cannot be launched.
+bool matmul_plan(dwm_matmul_plan& plan, int kernel, int splits)
 {
+    dwm_matmul_plan p = plan;
     const bool few = matmul_applies(p, kMatFew) && splits <= 1;
     p.shape = kernel >= 0 ? matmul_shape(p, kernel, kernel, splits) : matmul_shape(p, kMat64, few ? kMatFew : kMat256, splits);
+    if (p.shape.kernel < 0) return false;
     if (p.operands == DWM_PACKED || p.shape.kernel <= kMatAny64) {
         p.any = p.shape;
     } else if (kernel == kMatFew || (kernel < 0 && few && matmul_cost(p, kMatFewLoose, 1) < matmul_cost(p, kMatAny64, matmul_shape(p, kMatAny64, kMatAny64, splits).splits))) {
         p.any = {kMatFewLoose, 1};
     } else {
         p.any = matmul_shape(p, kMatAny, kMatAny64, splits);
+        if (p.any.kernel < 0) return false;
     }
     // Rows of odd lengths: the kernels for any alignment, or, where it costs less (or a kernel for aligned operands was asked for), copies and those for aligned ones
     // (bfloat16, us, without and with: 4001 x 4003 x 4005 350, 142; 1000 x 777 x 1021 16.3, 13.6, both across 22.7, 13.9; 300 x 300 x 500 8.3, 12.4).
@@ -171,6 +183,8 @@ void matmul_plan(dwm_matmul_plan& p, int kernel, int splits)
     p.copies = p.operands != DWM_PACKED && (a.odd() || b.odd()) && p.K > 0 && p.shape.kernel >= kMat64 && p.shape.kernel <= kMat256 && a.stride() <= 1 << 22 && b.stride() <= 1 << 22 &&
                (kernel >= 0 || matmul_cost(p, p.shape.kernel, p.shape.splits) + copies_cost(p) < matmul_cost(p, p.any.kernel, p.any.splits));
     if (p.operands != DWM_PACKED && (a.odd() || b.odd()) && p.K > 0 && !p.copies) p.shape = p.any;  // (no address or stride makes these whole vectors)
+    plan = p;
+    return true;
 }
 
 // Whether the kernels that copy sixteen bytes at a time straight into LDS can read an operand; a tile's 256 rows have to lie within 2^32 bytes.
@@ -551,11 +565,12 @@ dwm_status_t dwm_matmul_set_variant(dwm_matmul_plan_t* plan, const char* stage, 
     if (plan->ws) return DWM_ERR_WORKSPACE;
     if (kernel) {
         if (variant >= 0 && !matmul_applies(*plan, variant)) return DWM_ERR_INVALID_ARG;
-        plan->asked_kernel = variant < 0 ? -1 : variant;
-        matmul_plan(*plan, plan->asked_kernel, -1);
+        const int asked = variant < 0 ? -1 : variant;
+        if (!matmul_plan(*plan, asked, -1)) return DWM_ERR_INVALID_ARG;
+        plan->asked_kernel = asked;
     } else {
         if (variant == 0 || variant > 64 || (variant > 1 && plan->asked_kernel == kMatFew)) return DWM_ERR_INVALID_ARG;
-        matmul_plan(*plan, plan->asked_kernel, variant);
+        if (!matmul_plan(*plan, plan->asked_kernel, variant)) return DWM_ERR_INVALID_ARG;
     }
     return DWM_OK;
 }

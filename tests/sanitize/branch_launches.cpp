@@ -23,9 +23,12 @@ dwm_status_t launch_columns(const float*, int, int, void*, dwm_type_t, void*) { 
 dwm_status_t launch_aligned_rows(const AlignedRows*, int, void*) { return DWM_OK; }
 
 static MatmulShape launched;
+static bool too_many;  // threads: a launch has fewer than 2^32
 static dwm_status_t matmul(const MatmulArgs& a, int kernel)
 {
     launched = {kernel, a.splits};
+    const long long side = kernel == kMatAny64 || kernel == kMat64 ? 64 : kernel == kMat256 ? 256 : 128, threads = side == 256 ? 512 : 256;
+    too_many = kernel < kMatFew && (a.M + side - 1) / side * ((a.N + side - 1) / side) * a.splits * threads >= 1LL << 32;
     return DWM_OK;
 }
 dwm_status_t launch_matmul_f16(const MatmulArgs& a, int, int kernel, void*) { return matmul(a, kernel); }
@@ -76,6 +79,26 @@ int main(int argc, char** argv)
             const int kernel = dwm::launched.kernel == dwm::kMatFewLoose ? (int)dwm::kMatFew : dwm::launched.kernel;
             require(kernel == info.kernel && dwm::launched.splits == info.splits, "another kernel than the plan says", info, flags, operands);
         }
+        dwm_matmul_plan_destroy(plan);
+    }
+    // The largest results, operands aligned and not, as planned and as asked for: what a plan takes can be launched.
+    for (int i = 0; i < rounds; ++i) {
+        const int few = (int)upto(1), flags = (int)upto(3), e = upto(1) ? 8 : 1, M = (int)(few ? size(24) : (1 << 24) - size(23)) / e * e, N = (int)((1LL << 37) / (M > 0 ? M : 1) > 1 << 24 ? size(24) : (1LL << 37) / (M > 0 ? M : 1) - size(10));
+        const dwm_type_t operands = flags ? DWM_BF16 : (dwm_type_t)(1 + upto(2));
+        dwm_matmul_plan_t* plan = nullptr;
+        if (M <= 0 || N <= 0 || dwm_matmul_plan_create(&plan, M, N / e * e, size(16), operands, operands == DWM_PACKED ? DWM_F16 : operands, DWM_F32, DWM_ACT_NONE, flags) != DWM_OK) continue;
+        if (!upto(2)) dwm_matmul_set_variant(plan, "kernel", (int)upto(6) - 1);
+        if (!upto(2)) dwm_matmul_set_variant(plan, "splits", (int)upto(65) - 1);
+        const size_t bytes = dwm_matmul_workspace_bytes(plan);
+        if (bytes) dwm_matmul_set_workspace(plan, kSpace, bytes);
+        dwm_matmul_info_t info;
+        if (dwm_matmul_plan_info(plan, &info) != DWM_OK) return 1;
+        if (info.M > 0 && info.N > 0)
+            for (int which = 0; which < 4; ++which) {
+                require(call(plan, operands, which & 1 ? loose : good, which & 2 ? loose : good) == DWM_OK, "a large call", info, flags, operands);
+                require(!dwm::too_many, "more threads than a launch has", info, flags, operands);
+                ++run;
+            }
         dwm_matmul_plan_destroy(plan);
     }
     std::printf("branch launches: %d rounds, %lld calls\n", rounds, run);
