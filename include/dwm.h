@@ -664,7 +664,7 @@ typedef struct {
 
 /* operands: DWM_F16 or DWM_BF16, with type (that of out and residual) the same or DWM_F32; or DWM_PACKED, with type DWM_F16 or
  * DWM_BF16 and flags 0.  param_type (of bias) is DWM_F32, or the operands' 16-bit type (packed operands: type).  M, N >= 0 (0: nothing to do), K >= 0 (0: p = bias).  DWM_ERR_UNSUPPORTED for M, N or K above
- * 2^24, M * N above 2^37, or other types.  Host only. */
+ * 2^24, M * N above 2^37, other types, or packed operands that dwm_pack would refuse (K above 2^20); at the calls for packed results that it would (N above 2^20).  Host only. */
 DWM_API dwm_status_t dwm_matmul_plan_create(dwm_matmul_plan_t** out, int M, int N, int K, dwm_type_t operands, dwm_type_t type,
                                             dwm_type_t param_type, dwm_act_t act, int flags);
 DWM_API dwm_status_t dwm_matmul_plan_destroy(dwm_matmul_plan_t* plan);

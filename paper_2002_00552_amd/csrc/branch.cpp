@@ -12,7 +12,7 @@ bool known(dwm_type_t type) { return type == DWM_F32 || type == DWM_F16 || type 
 bool known(dwm_act_t act) { return act >= DWM_ACT_NONE && act <= DWM_ACT_SILU; }
 bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
-bool rows_fit(long long rows, long long C) { return C <= kMostChannels && rows <= kMostElements / C; }
+bool rows_fit(long long rows, long long C) { return C <= kMostChannels && (C == 0 || rows <= kMostElements / C); }
 
 // Packed rows that a call is given: there in whole, and where they have to lie.
 bool packed_ok(const dwm_packed_t* p) { return !p || (p->codes && p->scales && aligned(p->codes, 16) && aligned(p->scales, 4)); }
@@ -223,11 +223,13 @@ dwm_status_t run_matmul(const dwm_matmul_plan& p, MatmulArgs& a, const MatmulSha
 }
 
 // What both matmul calls ask of everything but the operands.
-bool matmul_ok(const dwm_matmul_plan& p, const void* bias, const void* residual, const void* out, const dwm_packed_t* packed_y,
-               const dwm_packed_t* kept)
+dwm_status_t matmul_ok(const dwm_matmul_plan& p, const void* bias, const void* residual, const void* out, const dwm_packed_t* packed_y,
+                       const dwm_packed_t* kept)
 {
-    return (out || packed_y || kept || p.M == 0 || p.N == 0) && aligned(bias, size_of(p.param_type)) && aligned(residual, size_of(p.type)) &&
-           aligned(out, size_of(p.type)) && packed_ok(packed_y) && packed_ok(kept);
+    if (!(out || packed_y || kept || p.M == 0 || p.N == 0) || !aligned(bias, size_of(p.param_type)) || !aligned(residual, size_of(p.type)) ||
+        !aligned(out, size_of(p.type)) || !packed_ok(packed_y) || !packed_ok(kept))
+        return DWM_ERR_INVALID_ARG;
+    return (packed_y || kept) && !rows_fit(p.M, p.N) ? DWM_ERR_UNSUPPORTED : DWM_OK;
 }
 
 const char* const kRmsNames[kRmsTensors] = {"x", "residual", "z", "y", "dy", "dz", "dx"};
@@ -510,6 +512,7 @@ dwm_status_t dwm_matmul_plan_create(dwm_matmul_plan_t** out, int M, int N, int K
         return DWM_ERR_INVALID_ARG;
     if (operands == DWM_F32 || (operands == DWM_PACKED ? type == DWM_F32 || flags : type != DWM_F32 && type != operands)) return DWM_ERR_UNSUPPORTED;
     if (M > most || N > most || K > most || (long long)M * N > kMostElements >> 3) return DWM_ERR_UNSUPPORTED;
+    if (operands == DWM_PACKED && (!rows_fit(M, K) || !rows_fit(N, K))) return DWM_ERR_UNSUPPORTED;  // (rows that dwm_pack does not make)
     dwm_matmul_plan* p = new (std::nothrow) dwm_matmul_plan;
     if (!p) return DWM_ERR_ALLOC;
     std::memset(p, 0, sizeof(*p));
@@ -591,9 +594,11 @@ dwm_status_t dwm_matmul_set_workspace(dwm_matmul_plan_t* plan, void* ws_dev, siz
 dwm_status_t dwm_matmul(const dwm_matmul_plan_t* plan, const void* a_dev, const void* b_dev, const void* bias_dev, const void* residual_dev,
                         void* out_dev, const dwm_packed_t* y_packed, const dwm_packed_t* kept, void* stream)
 {
-    if (!plan || plan->operands == DWM_PACKED || !matmul_ok(*plan, bias_dev, residual_dev, out_dev, y_packed, kept)) return DWM_ERR_INVALID_ARG;
+    if (!plan || plan->operands == DWM_PACKED) return DWM_ERR_INVALID_ARG;
     const bool some = plan->M > 0 && plan->N > 0;
     if ((some && plan->K > 0 && (!a_dev || !b_dev)) || !aligned(a_dev, 2) || !aligned(b_dev, 2)) return DWM_ERR_INVALID_ARG;
+    const dwm_status_t ok = matmul_ok(*plan, bias_dev, residual_dev, out_dev, y_packed, kept);
+    if (ok != DWM_OK) return ok;
     if (!some) return DWM_OK;
     MatmulArgs a{};
     a.a = a_dev;
@@ -633,10 +638,11 @@ dwm_status_t dwm_matmul(const dwm_matmul_plan_t* plan, const void* a_dev, const 
 dwm_status_t dwm_matmul_packed(const dwm_matmul_plan_t* plan, const dwm_packed_t* a, const dwm_packed_t* b, const void* bias_dev,
                                const void* residual_dev, void* out_dev, const dwm_packed_t* y_packed, const dwm_packed_t* kept, void* stream)
 {
-    if (!plan || plan->operands != DWM_PACKED || !matmul_ok(*plan, bias_dev, residual_dev, out_dev, y_packed, kept) || !packed_ok(a) || !packed_ok(b))
-        return DWM_ERR_INVALID_ARG;
+    if (!plan || plan->operands != DWM_PACKED || !packed_ok(a) || !packed_ok(b)) return DWM_ERR_INVALID_ARG;
     const bool some = plan->M > 0 && plan->N > 0;
     if (some && plan->K > 0 && (!a || !b)) return DWM_ERR_INVALID_ARG;
+    const dwm_status_t ok = matmul_ok(*plan, bias_dev, residual_dev, out_dev, y_packed, kept);
+    if (ok != DWM_OK) return ok;
     if (!some) return DWM_OK;
     MatmulArgs args{};
     if (a && b) {

@@ -71,3 +71,32 @@ def test_parts_where_few_rows_have_a_kernel_of_their_own():
         with pytest.raises(dwm.DwmError) as e:
             dwm.dwm_matmul_set_variant(plan, "splits", 3)
         assert e.value.status == dwm.DWM_ERR_INVALID_ARG
+
+
+def refused(status, f, *args):
+    with pytest.raises(dwm.DwmError) as e:
+        f(*args)
+    assert e.value.status == status
+
+
+@pytest.mark.parametrize("M, N, K", [(8, 8, (1 << 20) + 1), (1, 1, 1 << 24), (1 << 24, 8, 1 << 17), (8, 1 << 24, 1 << 17)])
+def test_packed_operands_that_cannot_be_made_are_refused(M, N, K):
+    assert dwm.dwm_packed_codes_bytes(M, K) == 0 or dwm.dwm_packed_codes_bytes(N, K) == 0
+    refused(dwm.DWM_ERR_UNSUPPORTED, dwm.dwm_matmul_plan_create, M, N, K, dwm.DWM_PACKED, dwm.DWM_BF16, dwm.DWM_F32, 0, 0)
+
+
+@pytest.mark.parametrize("M, N, K", [(8, 8, 1 << 20), (1 << 20, 16, 1 << 20), (8, 8, 0)])
+def test_the_largest_packed_operands(M, N, K):
+    with Product(M, N, K, operands=dwm.DWM_PACKED):
+        pass
+
+
+@pytest.mark.parametrize("operands", [dwm.DWM_BF16, dwm.DWM_PACKED])
+def test_packed_results_that_cannot_be_sized_are_refused(operands):
+    N, rows = (1 << 20) + 1, dwm.dwm_packed_t(ONE, ONE)
+    with Product(4, N, 64, operands=operands) as plan:
+        assert dwm.dwm_packed_codes_bytes(4, N) == 0
+        f, a = (dwm.dwm_matmul_packed, rows) if operands == dwm.DWM_PACKED else (dwm.dwm_matmul, ONE)
+        for packed in ((rows, None), (None, rows)):
+            refused(dwm.DWM_ERR_UNSUPPORTED, f, plan, a, a, None, None, ONE, *packed)
+            refused(dwm.DWM_ERR_UNSUPPORTED, f, plan, a, a, None, None, None, *packed)
