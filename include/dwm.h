@@ -604,7 +604,8 @@ DWM_API dwm_status_t dwm_rms_set_variant(dwm_rms_plan_t* plan, const char* stage
 /* The workspace holds partial sums of dgamma: 256-byte aligned, needed by backward calls that are asked for it and by no other. */
 DWM_API size_t dwm_rms_workspace_bytes(const dwm_rms_plan_t* plan);
 DWM_API dwm_status_t dwm_rms_set_workspace(dwm_rms_plan_t* plan, void* ws_dev, size_t bytes);
-/* residual NULL: z is x, and z_dev has to be NULL.  gamma may be NULL (ones); any of z, y, y_packed (y in 8 bits, from binary32),
+/* residual NULL: z is x, and z_dev has to be NULL.  gamma may be NULL (ones); any of z, y, y_packed (y in 8 bits: the codes of the
+ * exact z * rstd * gamma, so that they may differ from dwm_pack's of y where binary32 rounds y onto the border between two codes or scales),
  * kept (z in 8 bits, as it is stored) and rstd ([rows]) may be NULL, but not all of them.  z may be residual or x, y may be x. */
 DWM_API dwm_status_t dwm_rms_forward(const dwm_rms_plan_t* plan, const void* x_dev, const void* residual_dev, const void* gamma_dev,
                                      void* z_dev, void* y_dev, const dwm_packed_t* y_packed, const dwm_packed_t* kept,

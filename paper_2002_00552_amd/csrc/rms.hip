@@ -76,12 +76,13 @@ __device__ __forceinline__ Rstd rms_rstd(double sum, const RmsArgs& a)
     return {hi, hi < 3e38f ? (float)(r - (double)hi) : 0.0f};
 }
 
-// Whether a number lies right between two codes, or is the largest that a scale holds: one in some 2^20 does once it is rounded to binary32, which side the
-// exact value is on then decides, and not the tie.
+// Whether a number may lie right between two codes, or be the largest that a scale holds: some do once they are rounded to binary32, and then the side that the
+// exact value is on decides, not the tie.  Borders have at most four bits behind the first (between two codes of three: four; 448: two; odd multiples of 2^-10, between the
+// codes below the smallest binade, three), so one value in 2^19 is looked at; numbers of so few bits that are no borders are as near to their code a step of binary32 further.
 __device__ __forceinline__ bool on_border(float y)
 {
-    const uint32_t u = __float_as_uint(y);
-    return (u & 0xfffffu) == 0x80000u || (u & 0x7fffffu) == 0x600000u;
+    const uint32_t u = __float_as_uint(y) & 0x7fffffffu;
+    return (u & 0x7ffffu) == 0u && u - 1u < kInfinity - 1u;  // (no zero, infinity or NaN)
 }
 
 // What a row's octet leaves behind: z, y and both in 8 bits.
