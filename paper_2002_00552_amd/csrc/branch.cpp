@@ -297,7 +297,7 @@ dwm_status_t dwm_rms_plan_create(dwm_rms_plan_t** out, long long rows, int C, dw
     p->C = C;
     p->type = type;
     p->param_type = param_type;
-    p->eps = (float)eps;
+    p->eps = eps;
     for (long long& s : p->stride) s = C;
     p->forward = rms_choice(C, false);
     p->backward = rms_choice(C, true);

@@ -30,7 +30,7 @@ struct RmsArgs {
     long long stride[kRmsTensors];
     long long rows;
     int C, param_typed, splits;
-    float eps;
+    double eps;
 };
 // Threads of a row, octets of a thread, and in which directions the shape is built; variant i + 1 is entry i.
 struct RmsShape {
@@ -105,7 +105,7 @@ struct dwm_rms_plan {
     long long rows;
     int C;
     dwm_type_t type, param_type;
-    float eps;
+    double eps;
     long long stride[dwm::kRmsTensors];
     int forward, backward, splits;
     void* ws;

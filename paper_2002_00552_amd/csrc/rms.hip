@@ -68,7 +68,7 @@ struct Rstd {
 };
 __device__ __forceinline__ Rstd rms_rstd(double sum, const RmsArgs& a)
 {
-    const double m = sum / (double)a.C + (double)a.eps;
+    const double m = sum / (double)a.C + a.eps;
     double r = __builtin_amdgcn_rsq(m);
     const double better = r * (1.5 - 0.5 * m * r * r);
     r = better > 0.0 && m > 0.0 ? better : r;  // (zero, infinity and NaN as they are)

@@ -78,3 +78,13 @@ def test_codes_of_many_values(dtype):
     norm = Norm(z, (1 + 0.2 * rng.standard_normal(C)).astype(np.float32), 1e-5, dtype)
     norm.check_codes()
     norm.check_values(dtype)
+
+
+@pytest.mark.parametrize("eps", [1e-5, 1e-6, 3e-7, 1e-12])
+def test_eps_counts_in_64_bits(eps):
+    """Rows far below the root of eps, which rstd then comes from."""
+    for seed in range(4):
+        z, gamma = rows_on_borders(4096, eps, 1e-3 * np.sqrt(eps), NORMAL, seed)
+        norm = Norm(z, gamma, eps)
+        norm.check_codes()
+        norm.check_values()
