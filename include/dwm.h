@@ -579,7 +579,7 @@ DWM_API dwm_status_t dwm_unpack(dwm_type_t type, long long rows, int C, const dw
 /*
  * Root-mean-square norm, with the addition of a residual in front of it:
  *     z = residual + x (rounded to binary32, then to its type), rstd = 1 / sqrt((1/C) sum_c z^2 + eps), y = z * rstd * gamma[c]
- * the norm reads z as it is stored.  Values of up to about 1e19 / sqrt(C) can be normed; an infinity or NaN spoils its own row alone.
+ * the norm reads z as it is stored.  Rows whose 1 / rstd lies between 2^-126 and 2^125 can be normed; an infinity or NaN spoils its own row alone.
  */
 typedef struct dwm_rms_plan dwm_rms_plan_t;
 typedef struct {

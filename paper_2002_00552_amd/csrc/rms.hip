@@ -97,12 +97,12 @@ __device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int o
         store_packed(a.kept, row, octet, a.C, codes, s);
     }
     if (!a.y && !a.packed_y.codes) return;
-    float y[8], t[8], rest[8];  // y = t * hi + rest, t * hi rounded with it: one rounding
+    float y[8], t[8], rest[8];  // y = t * gamma + rest with t = z * hi, what that rounding lost and lo in rest: one rounding; z * rstd first, which is at most sqrt(C), where z * gamma might leave binary32
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        t[j] = z[j] * gamma[j];
-        rest[j] = fmaf(t[j], rstd.lo, fmaf(z[j], gamma[j], -t[j]) * rstd.hi);
-        y[j] = fmaf(t[j], rstd.hi, rest[j]);
+        t[j] = z[j] * rstd.hi;
+        rest[j] = fmaf(z[j], rstd.lo, fmaf(z[j], rstd.hi, -t[j])) * gamma[j];
+        y[j] = fmaf(t[j], gamma[j], rest[j]);
     }
     if (a.y && n > 0) store_octet<T>((T*)a.y + row * a.stride[kRmsY] + c, n, y);
     if (a.packed_y.codes) {
@@ -115,7 +115,7 @@ __device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int o
         if (border)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float off = fmaf(t[j], rstd.hi, -y[j]) + rest[j];
+                const float off = fmaf(t[j], gamma[j], -y[j]) + rest[j];
                 if (j < n && on_border(y[j]) && off != 0.0f) y[j] = __uint_as_float(__float_as_uint(y[j]) + ((off > 0.0f) == (y[j] > 0.0f) ? 1 : -1));
             }
         uint32_t s;

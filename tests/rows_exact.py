@@ -34,5 +34,6 @@ def norm(z, gamma, eps):
 
 # The squares of binary32 numbers are exact in 64 bits, and so are sums of them to some C 2^-53; what is left is one rounding to binary32, a second word of rstd that is rounded
 # itself (2^-48), and a product of that word and the first one's remainder with roundings of 2^-24 of some 2^-24: 2^-10 of a rounding holds all of that.  The smallest number beside it.
-def one_rounding(value):
-    return (1 + 2.0 ** -10) * U * np.abs(value) + 2.0 ** -149
+# A second word of rstd below 2^-126 is rounded to a multiple of 2^-149: 2^-150 off, and y = z rstd gamma by |z gamma| 2^-150 = |y| 2^-150 / rstd (nothing but for roots near 2^125).
+def one_rounding(value, rstd=1.0):
+    return (1 + 2.0 ** -10) * U * np.abs(value) + 2.0 ** -149 + np.abs(value) * 2.0 ** -150 / rstd

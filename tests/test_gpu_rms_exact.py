@@ -34,7 +34,7 @@ class Norm:
         assert not differ.any(), "%d of %d codes differ, the first at %s" % (differ.sum(), codes.size, np.argwhere(differ)[0])
 
     def check_values(self, dtype="f32"):
-        tolerance = exact.one_rounding(self.want)
+        tolerance = exact.one_rounding(self.want, self.root[:, None])
         within(self.y.numpy(), self.want, tolerance + (0 if dtype == "f32" else ref.stored(self.want, dtype)), "y")
         within(self.rstd.double().cpu().numpy(), self.root, exact.one_rounding(self.root), "rstd")
 
@@ -88,3 +88,14 @@ def test_eps_counts_in_64_bits(eps):
         norm = Norm(z, gamma, eps)
         norm.check_codes()
         norm.check_values()
+
+
+@pytest.mark.parametrize("variant", [-1, 0])
+@pytest.mark.parametrize("size, by", [(1e-30, 1e-10), (1e-36, 1e-4), (1e30, 1e12), (1e37, 1e5), (1e-12, 1e30), (1e12, 1e-30)])
+def test_far_rows_and_far_gammas(size, by, variant):
+    """z * gamma leaves binary32, y does not."""
+    rng = np.random.default_rng(3)
+    z = (size * rng.standard_normal((5, 700))).astype(np.float32)
+    norm = Norm(z, (by * (1 + rng.random(700))).astype(np.float32), 0.0, variant=variant)
+    norm.check_values()
+    norm.check_codes()
