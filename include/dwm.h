@@ -599,7 +599,7 @@ DWM_API dwm_status_t dwm_rms_plan_info(const dwm_rms_plan_t* plan, dwm_rms_info_
 DWM_API dwm_status_t dwm_rms_set_stride(dwm_rms_plan_t* plan, const char* tensor, long long stride);
 /* A kernel by number, for tuning and tests: stage "forward" or "backward" (this one before dwm_rms_set_workspace only,
  * DWM_ERR_WORKSPACE afterwards); 0 = any size, 1 .. 14 = the library's internal table of threads of a row and octets of a thread,
- * negative: the planner's choice.  DWM_ERR_INVALID_ARG for one that does not hold C channels or is not built. */
+ * negative: the planner's choice.  DWM_ERR_INVALID_ARG for one that does not hold C channels. */
 DWM_API dwm_status_t dwm_rms_set_variant(dwm_rms_plan_t* plan, const char* stage, int variant);
 /* The workspace holds partial sums of dgamma: 256-byte aligned, needed by backward calls that are asked for it and by no other. */
 DWM_API size_t dwm_rms_workspace_bytes(const dwm_rms_plan_t* plan);

@@ -25,20 +25,20 @@ template <int N> int named(const char* const (&names)[N], const char* name)
     return -1;
 }
 
-bool rms_fits(int variant, int C, bool backward)
+bool rms_fits(int variant, int C)
 {
     if (variant < 1 || variant > kRmsShapeCount) return variant == 0;
     const RmsShape& s = kRmsShapes[variant - 1];
-    return s.tpr * s.k * kOctet >= C && (backward ? s.backward : s.forward);
+    return s.tpr * s.k * kOctet >= C;
 }
 
 // The narrowest shape that holds a row with one octet a thread, or, past 8192 channels, two (16384 rows of 4096 bfloat16, z and y: 256 threads with two octets 116 us,
 // 512 with one 109; backward 114 and 108).
-int rms_choice(int C, bool backward)
+int rms_choice(int C)
 {
     for (int octets = 1; octets <= 2; ++octets)
         for (int v = 1; v <= kRmsShapeCount; ++v)
-            if (rms_fits(v, C, backward) && kRmsShapes[v - 1].k == octets) return v;
+            if (rms_fits(v, C) && kRmsShapes[v - 1].k == octets) return v;
     return 0;
 }
 
@@ -299,8 +299,7 @@ dwm_status_t dwm_rms_plan_create(dwm_rms_plan_t** out, long long rows, int C, dw
     p->param_type = param_type;
     p->eps = eps;
     for (long long& s : p->stride) s = C;
-    p->forward = rms_choice(C, false);
-    p->backward = rms_choice(C, true);
+    p->forward = p->backward = rms_choice(C);
     p->splits = rms_splits(rows, C, p->backward);
     *out = p;
     return DWM_OK;
@@ -335,8 +334,8 @@ dwm_status_t dwm_rms_set_variant(dwm_rms_plan_t* plan, const char* stage, int va
     const bool backward = !std::strcmp(stage, "backward");
     if (!backward && std::strcmp(stage, "forward")) return DWM_ERR_INVALID_ARG;
     if (backward && plan->ws) return DWM_ERR_WORKSPACE;
-    const int v = variant < 0 ? rms_choice(plan->C, backward) : variant;
-    if (!rms_fits(v, plan->C, backward)) return DWM_ERR_INVALID_ARG;
+    const int v = variant < 0 ? rms_choice(plan->C) : variant;
+    if (!rms_fits(v, plan->C)) return DWM_ERR_INVALID_ARG;
     (backward ? plan->backward : plan->forward) = v;
     plan->splits = rms_splits(plan->rows, plan->C, plan->backward);
     return DWM_OK;

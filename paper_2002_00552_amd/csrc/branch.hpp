@@ -24,7 +24,7 @@ constexpr int kMostChannels = 1 << 20;
 enum RmsTensor { kRmsX, kRmsResidual, kRmsZ, kRmsY, kRmsDy, kRmsDz, kRmsDx, kRmsTensors };
 struct RmsArgs {
     const void *x, *residual, *gamma, *dy, *dz;
-    void *z, *y, *dx, *dgamma;
+    void *z, *y, *dx;
     Packed packed_y, kept;
     float *rstd, *partial;  // [rows], [splits][C]
     long long stride[kRmsTensors];
@@ -32,15 +32,14 @@ struct RmsArgs {
     int C, param_typed, splits;
     double eps;
 };
-// Threads of a row, octets of a thread, and in which directions the shape is built; variant i + 1 is entry i.
+// Threads of a row, octets of a thread; variant i + 1 is entry i, built forward and backward.  The planner takes those of one octet and, past 8192 channels, the last; the others are for
+// dwm_rms_set_variant alone.
 struct RmsShape {
     int tpr, k;
-    bool forward, backward;
+    static constexpr bool forward = true, backward = true;
 };
 constexpr RmsShape kRmsShapes[] = {
-    {4, 1, true, true},    {8, 1, true, true},   {16, 1, true, true},  {32, 1, true, true},   {64, 1, true, true},
-    {64, 2, true, true},   {128, 1, true, true}, {128, 2, true, true}, {256, 1, true, true},  {256, 2, true, true},
-    {512, 1, true, true},  {512, 2, true, true}, {1024, 1, true, true}, {1024, 2, true, true},
+    {4, 1}, {8, 1}, {16, 1}, {32, 1}, {64, 1}, {64, 2}, {128, 1}, {128, 2}, {256, 1}, {256, 2}, {512, 1}, {512, 2}, {1024, 1}, {1024, 2},
 };
 constexpr int kRmsShapeCount = sizeof(kRmsShapes) / sizeof(kRmsShapes[0]);
 
@@ -48,7 +47,7 @@ constexpr int kRmsShapeCount = sizeof(kRmsShapes) / sizeof(kRmsShapes[0]);
 enum ActTensor { kActX, kActY, kActDy, kActDx, kActTensors };
 struct ActArgs {
     const void *x, *bias, *dy;
-    void *y, *dx, *dbias;
+    void *y, *dx;
     Packed kept;
     float* partial;  // [splits][C]
     long long stride[kActTensors];

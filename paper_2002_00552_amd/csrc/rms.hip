@@ -1,5 +1,5 @@
 // Root-mean-square norms of rows with the addition of a residual (gfx950).  Memory bounds them: a row is read once and held in registers, an
-// octet of neighbouring channels to a thread (and one to three more, a row's threads further on), so that four lanes hold a block of
+// octet of neighbouring channels to a thread (and one more, a row's threads further on, in the widest rows), so that four lanes hold a block of
 // 32 channels and its scale comes out of two exchanges between neighbours.  A row's threads are a part of a wave, a wave or a
 // workgroup; the kernels for any size read a row twice.  Operands out of the caches, 16384 rows of 4096 bfloat16: z and y from x and residual 99 us (5.4 TB/s), the
 // gradient from z's checkpoint with dz and dgamma 85 us (5.5 TB/s) and 5 for the last sums; a copy of 1 GiB runs at 5.1 TB/s on the same card.
@@ -416,10 +416,7 @@ template <class T, int I> static dwm_status_t shaped(const RmsArgs& a, int kerne
     if constexpr (I < kRmsShapeCount) {
         constexpr RmsShape sh = kRmsShapes[I];
         if (kernel != I + 1) return shaped<T, I + 1>(a, kernel, backward, s);
-        if constexpr (sh.backward)
-            if (backward) return backward_shape<T, sh.tpr, sh.k>(a, s);
-        if constexpr (sh.forward)
-            if (!backward) return forward_shape<T, sh.tpr, sh.k>(a, s);
+        return backward ? backward_shape<T, sh.tpr, sh.k>(a, s) : forward_shape<T, sh.tpr, sh.k>(a, s);
     }
     return DWM_ERR_INVALID_ARG;
 }
