@@ -360,6 +360,7 @@ static RmsArgs rms_args(const dwm_rms_plan& p)
     a.param_typed = p.param_type == p.type && p.type != DWM_F32;
     a.splits = p.splits;
     a.eps = p.eps;
+    a.inverse = 1.0 / p.C;
     return a;
 }
 

@@ -30,7 +30,7 @@ struct RmsArgs {
     long long stride[kRmsTensors];
     long long rows;
     int C, param_typed, splits;
-    double eps;
+    double eps, inverse;  // 1 / C
 };
 // Threads of a row, octets of a thread; variant i + 1 is entry i, built forward and backward.  The planner takes those of one octet and, past 8192 channels, the last; the others are for
 // dwm_rms_set_variant alone.

@@ -68,7 +68,7 @@ struct Rstd {
 };
 __device__ __forceinline__ Rstd rms_rstd(double sum, const RmsArgs& a)
 {
-    const double m = sum / (double)a.C + a.eps;
+    const double m = fma(sum, a.inverse, a.eps);
     double r = __builtin_amdgcn_rsq(m);
     const double better = r * (1.5 - 0.5 * m * r * r);
     r = better > 0.0 && m > 0.0 ? better : r;  // (zero, infinity and NaN as they are)
@@ -78,12 +78,8 @@ __device__ __forceinline__ Rstd rms_rstd(double sum, const RmsArgs& a)
 
 // Whether a number may lie right between two codes, or be the largest that a scale holds: some do once they are rounded to binary32, and then the side that the
 // exact value is on decides, not the tie.  Borders have at most four bits behind the first (between two codes of three: four; 448: two; odd multiples of 2^-10, between the
-// codes below the smallest binade, three), so one value in 2^19 is looked at; numbers of so few bits that are no borders are as near to their code a step of binary32 further.
-__device__ __forceinline__ bool on_border(float y)
-{
-    const uint32_t u = __float_as_uint(y) & 0x7fffffffu;
-    return (u & 0x7ffffu) == 0u && u - 1u < kInfinity - 1u;  // (no zero, infinity or NaN)
-}
+// codes below the smallest binade, three), so the lowest 19 of one value in 2^19 are zeros; numbers of so few bits that are no borders are as near to their code a step of binary32 further.
+__device__ __forceinline__ uint32_t off_border(float y) { return __float_as_uint(y) & 0x7ffffu; }
 
 // What a row's octet leaves behind: z, y and both in 8 bits.
 template <class T>
@@ -109,14 +105,15 @@ __device__ __forceinline__ void rms_write(const RmsArgs& a, long long row, int o
         if (n < 8)
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = j < n ? y[j] : 0.0f;  // (an infinite rstd makes NaN of zeros)
-        bool border = false;
+        uint32_t least = ~0u;  // (one question for the octet)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) border |= on_border(y[j]);
-        if (border)
+        for (int j = 0; j < 8; ++j) least = min(least, off_border(y[j]));
+        if (least == 0)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float off = fmaf(t[j], gamma[j], -y[j]) + rest[j];
-                if (j < n && on_border(y[j]) && off != 0.0f) y[j] = __uint_as_float(__float_as_uint(y[j]) + ((off > 0.0f) == (y[j] > 0.0f) ? 1 : -1));
+                const bool number = (__float_as_uint(y[j]) & 0x7fffffffu) - 1u < kInfinity - 1u;  // (no zero, infinity or NaN)
+                if (j < n && number && off_border(y[j]) == 0 && off != 0.0f) y[j] = __uint_as_float(__float_as_uint(y[j]) + ((off > 0.0f) == (y[j] > 0.0f) ? 1 : -1));
             }
         uint32_t s;
         const uint2v codes = pack_octet<QuadLanes>(y, &s);
